@@ -60,7 +60,7 @@
 extern "C" {
 #endif
 
-#define BNN_ABI_VERSION 8
+#define BNN_ABI_VERSION 9
 
 typedef enum bnn_status {
   BNN_OK = 0,
@@ -464,6 +464,190 @@ bnn_status bnn_bgemm(int64_t M, int64_t N, int64_t K, const uint32_t* A,
                      const uint32_t* B, const int32_t* thr,
                      const uint32_t* flip, int32_t* out_sums,
                      uint32_t* out_bits, hipStream_t stream);
+
+/* ------------------------------------------- mixtures of binary experts -- */
+/*
+ * A layer of E binary FC layers ("experts") of which every row takes top_k:
+ * bnn_route picks them from a router's scores, bnn_group_rows puts the (row,
+ * expert) pairs in expert order, bnn_experts_fc runs every pair's binary FC
+ * layer to bits and bnn_experts_sum the last one to a weighted sum per row.
+ * bnn_bgemm_lora is a binary FC layer that all rows share, with real-valued
+ * low-rank adapters per row beside it.  Not part of the paper; the binary
+ * products are those of Eq. 4.  Inference only: no call has a gradient.
+ */
+
+/* Element types of real-valued buffers. */
+typedef enum bnn_dtype {
+  BNN_F32 = 0,
+  BNN_F16 = 1,
+  BNN_BF16 = 2,
+  BNN_I32 = 3 /* int32 sums, e.g. of bnn_bgemm (bnn_route only) */
+} bnn_dtype;
+
+typedef enum bnn_score {
+  BNN_SCORE_SOFTMAX = 0, /* p_e = exp(z_e) / sum over the row's experts      */
+  BNN_SCORE_SIGMOID = 1  /* p_e = 1 / (1 + exp(-z_e))                        */
+} bnn_score;
+
+/* Limits of the calls below. */
+#define BNN_MAX_EXPERTS 1024
+#define BNN_MAX_TOP_K 16
+#define BNN_MAX_ROUTE_GROUPS 64
+#define BNN_MAX_RANK 256
+
+typedef struct bnn_route_desc {
+  int32_t E;          /* experts, 1..BNN_MAX_EXPERTS                         */
+  int32_t top_k;      /* experts per row, 1..min(BNN_MAX_TOP_K, E)           */
+  int32_t groups;     /* groups of E / groups consecutive experts: 1..64,    */
+                      /* dividing E                                          */
+  int32_t top_groups; /* groups that a row may choose from, 1..groups        */
+  int32_t group_top;  /* a group's score sums its 1 or 2 largest keys        */
+  int32_t score;      /* bnn_score                                           */
+  int32_t renorm;     /* 1: the chosen experts' p are divided by their sum   */
+  int32_t dtype;      /* bnn_dtype of the logits                             */
+  float scale;        /* factor on the weights                               */
+  float logit_scale;  /* factor on the logits, positive and finite           */
+} bnn_route_desc;
+
+/*
+ * Routing.  For row t and expert e, in fp32:
+ *   z_e = logit_scale * logits[t][e];  p_e as in bnn_score;
+ *   key_e = p_e + bias[e]  (bias NULL: key_e = p_e).
+ * An expert is out of reach of the row where its logit is -inf or NaN, or its
+ * key is -inf or NaN (a logit of +inf counts as the largest finite value, a
+ * finite one keeps its expert in reach, the type's lowest value too); it adds
+ * nothing to the softmax's sum.  With groups > 1, a group's score is the sum
+ * of its group_top largest keys (fewer in reach: their sum; none: lowest of
+ * all), and only the experts of the top_groups groups of the largest scores
+ * stay in reach.  ids[t] are the top_k experts of the largest keys in
+ * descending order; equal keys, and equal group scores, go to the lowest
+ * index.  weights[t][j] = scale * p of expert ids[t][j], divided by the sum
+ * of the row's chosen p with renorm (0 where that sum is 0).  Where fewer
+ * than top_k experts are in reach (a padding row: none), the places left hold
+ * id -1 and weight 0.  exp and the sums are in fp32, so keys that differ by
+ * less than a few units in the last place may come in either order.
+ *   logits  [T][E], rows `stride` elements apart (stride >= E), of d->dtype.
+ *   bias    [E] fp32 or NULL.
+ *   ids     [T][top_k] int32.   weights [T][top_k] fp32.
+ * T >= 0 (0 launches nothing).  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE (also a
+ * logits pointer not aligned to its element), BNN_ERR_HIP.
+ */
+bnn_status bnn_route(const bnn_route_desc* d, int64_t T, const void* logits,
+                     int64_t stride, const float* bias, int32_t* ids,
+                     float* weights, hipStream_t stream);
+
+/*
+ * Rows in the order of their group (a stable sort by ids).
+ *   ids      [M] int32; a row whose id is not in [0, G) is in no group.
+ *   offsets  [G + 1] int32: offsets[g] = rows with an id in [0, g).
+ *   order    [M] int32: the rows of group g at offsets[g] .. offsets[g + 1]
+ *            - 1 in ascending order, then from offsets[G] on the rows of no
+ *            group, in ascending order.
+ * 1 <= G <= BNN_MAX_EXPERTS, 0 <= M < 2^24 (M == 0 writes the offsets only).
+ * Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_HIP.
+ */
+bnn_status bnn_group_rows(int64_t M, int32_t G, const int32_t* ids,
+                          int32_t* offsets, int32_t* order, hipStream_t stream);
+
+typedef struct bnn_experts_desc {
+  int64_t T;         /* rows (tokens)                                        */
+  int32_t top_k;     /* experts per row, 1..BNN_MAX_TOP_K                    */
+  int32_t E;         /* experts, 1..BNN_MAX_EXPERTS                          */
+  int32_t N, K;      /* outputs and input bits of each expert                */
+  int32_t share;     /* rows of x: T (1: a row's experts read the same bits) */
+                     /* or T * top_k (0: bits of their own)                  */
+} bnn_experts_desc;
+
+/*
+ * Binary FC layers of the experts, to bits.  Pair m = t * top_k + j:
+ *   S[m][n] = dot of x row (share ? t : m) and w[e][n], e the pair's expert,
+ *   out bit = (S[m][n] >= thr[e][n]) XOR flip bit n of expert e.
+ * Bits of a pair without an expert are 0, and so are tail bits.
+ *   x        [T or T * top_k][Kw] u32, Kw = ceil(K / 32).
+ *   w        [E][N][Kw] u32.  thr [E][N] int32.  flip [E][ceil(N / 32)] u32
+ *            or NULL.
+ *   offsets, order   of bnn_group_rows over the T * top_k ids.  Entries out of
+ *            range are clamped into it, so that no access leaves the buffers.
+ *   out_bits [T * top_k][ceil(N / 32)] u32.
+ * T >= 0 (0 launches nothing), T * top_k < 2^24, N <= 65536, K <= 65535.
+ * x, w and out_bits 16-byte aligned.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE,
+ * BNN_ERR_ALIGN, BNN_ERR_HIP.
+ */
+bnn_status bnn_experts_fc(const bnn_experts_desc* d, const uint32_t* x,
+                          const uint32_t* w, const int32_t* offsets,
+                          const int32_t* order, const int32_t* thr,
+                          const uint32_t* flip, uint32_t* out_bits,
+                          hipStream_t stream);
+
+/*
+ * Binary FC layers of the experts, weighted and added up per row:
+ *   y[t][n] = sum over j < top_k of
+ *             weights[t][j] * alpha[e][n] * S[t * top_k + j][n]
+ * with e = ids[t][j] and S as above, added in fp32 in the order of j and
+ * rounded once to dtype; a pair whose id is not in [0, E) adds nothing (its
+ * weight is not read).  alpha NULL: all 1.
+ *   ids, weights   [T][top_k] int32 and fp32.
+ *   offsets, order   of bnn_group_rows over ids, which they must match.
+ *   alpha    [E][N] fp32 or NULL.
+ *   dtype    bnn_dtype of y: BNN_F32, BNN_F16 or BNN_BF16.
+ *   y        [T][N].
+ *   workspace (device, 16-byte aligned, ws_bytes >= the size that
+ *            bnn_experts_sum_workspace_size gives; needs no initialization).
+ * Sizes, alignment (x, w, y) and errors as for bnn_experts_fc, plus
+ * BNN_ERR_WORKSPACE.
+ */
+bnn_status bnn_experts_sum_workspace_size(const bnn_experts_desc* d,
+                                          size_t* bytes);
+bnn_status bnn_experts_sum(const bnn_experts_desc* d, const uint32_t* x,
+                           const uint32_t* w, const int32_t* ids,
+                           const float* weights, const int32_t* offsets,
+                           const int32_t* order, const float* alpha,
+                           int32_t dtype, void* y, void* workspace,
+                           size_t ws_bytes, hipStream_t stream);
+
+typedef struct bnn_lora_desc {
+  int64_t M;         /* rows                                                 */
+  int32_t N, K;      /* outputs, inputs                                      */
+  int32_t adapters;  /* low-rank adapters, 1..BNN_MAX_EXPERTS                */
+  int32_t rank;      /* their rank, a multiple of 8, 8..BNN_MAX_RANK         */
+                     /* (a smaller one: padded with zeros)                   */
+  int32_t dtype;     /* of x, a and b: BNN_F32, BNN_F16 or BNN_BF16          */
+  int32_t out_dtype; /* of y, the same                                       */
+} bnn_lora_desc;
+
+/*
+ * A binary FC layer shared by all rows, with a low-rank adapter per row:
+ *   y[m][n] = alpha[n] * S[m][n] + scale[l] * sum_r u[m][r] * b[l][n][r],
+ *   S[m][n] = dot of the +-1 values (x[m][k] + offset[k] > 0) and w[n]
+ *             (bnn_pack_bits, then Eq. 4),
+ *   u[m][r] = sum_k x[m][k] * a[l][r][k],   l = ids[m];
+ * a row whose id is not in [0, adapters) has the first term only.  Products
+ * with u and their sums are held in fp32 or better and y is rounded once.
+ * x must be finite; with one that is not, its row of y is unspecified (other
+ * rows are not touched by it).
+ *   x        [M][K], rows x_stride elements apart (x_stride >= K).
+ *   offset   [K] fp32 or NULL (0).
+ *   w        [N][Kw] u32 packed weights.   alpha [N] fp32 or NULL (1).
+ *   ids      [M] int32.
+ *   a        [adapters][rank][K], b [adapters][N][rank].
+ *   scale    [adapters] fp32 or NULL (1).
+ *   order    [M] int32, a permutation of the rows (bnn_group_rows of ids), or
+ *            NULL (rows as they come).  It never changes a result; rows of
+ *            one adapter that are far apart are quicker with it.  Entries out
+ *            of range are clamped into it.
+ *   y        [M][N].
+ *   workspace as for bnn_experts_sum.
+ * M >= 0 (0 launches nothing), M < 2^24, N <= 65536, K <= 65536.  x, w, a, b
+ * and y 16-byte aligned.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN,
+ * BNN_ERR_UNSUPPORTED (rank), BNN_ERR_WORKSPACE, BNN_ERR_HIP.
+ */
+bnn_status bnn_bgemm_lora_workspace_size(const bnn_lora_desc* d, size_t* bytes);
+bnn_status bnn_bgemm_lora(const bnn_lora_desc* d, const void* x,
+                          int64_t x_stride, const float* offset,
+                          const uint32_t* w, const float* alpha,
+                          const int32_t* ids, const void* a, const void* b,
+                          const float* scale, const int32_t* order, void* y,
+                          void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------ layer chain */
 typedef enum bnn_layer_kind {

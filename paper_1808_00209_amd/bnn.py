@@ -39,6 +39,8 @@ EXPORTED = ["bnn_last_error", "bnn_abi_version", "bnn_default_options", "bnn_set
             "bnn_bconv2d_prepared", "bnn_fconv2d_binw", "bnn_binarize_input", "bnn_bconv2d_input",
             "bnn_fconv_bconv2d", "bnn_input_bconv_bconv2d", "bnn_bconv_bconv2d", "bnn_bfc_pair", "bnn_bfc_tail",
             "bnn_bgemm",
+            "bnn_route", "bnn_group_rows", "bnn_experts_fc", "bnn_experts_sum_workspace_size",
+            "bnn_experts_sum", "bnn_bgemm_lora_workspace_size", "bnn_bgemm_lora",
             "bnn_forward_workspace_size", "bnn_forward", "bnn_forward_noalloc"]
 
 # Bytes of bnn_forward_noalloc's per-GPU scratch array (BNN_FORWARD_SCRATCH_BYTES).
@@ -76,6 +78,22 @@ class Layer(ctypes.Structure):
                 ("pad", ctypes.c_int32), ("pool", ctypes.c_int32), ("K", ctypes.c_int32),
                 ("N", ctypes.c_int32), ("w", ctypes.c_void_p), ("thr", ctypes.c_void_p),
                 ("flip", ctypes.c_void_p), ("offset", ctypes.c_void_p), ("wprep", ctypes.c_void_p)]
+
+
+class RouteDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("E", "top_k", "groups", "top_groups", "group_top", "score", "renorm", "dtype")]
+    _fields_ += [("scale", ctypes.c_float), ("logit_scale", ctypes.c_float)]
+
+
+class ExpertsDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in
+                                          ("top_k", "E", "N", "K", "share")]
+
+
+class LoraDesc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in
+                                          ("N", "K", "adapters", "rank", "dtype", "out_dtype")]
 
 
 _lib = None
@@ -117,6 +135,17 @@ def load(path: str = LIB_PATH):
                                       P, P, P, P, P, P, P, P, P]
     lib.bnn_bfc_pair.argtypes = [i64, i64, i64, i64, P, P, P, P, P, P, P, P, P, P]
     lib.bnn_bfc_tail.argtypes = [i64, i64, i64, i64, P, P, P, P, P, P, P, P, P, P, P]
+    lib.bnn_route.argtypes = [ctypes.POINTER(RouteDesc), i64, P, i64, P, P, P, P]
+    lib.bnn_group_rows.argtypes = [i64, i32, P, P, P, P]
+    lib.bnn_experts_fc.argtypes = [ctypes.POINTER(ExpertsDesc), P, P, P, P, P, P, P, P]
+    lib.bnn_experts_sum_workspace_size.argtypes = [ctypes.POINTER(ExpertsDesc),
+                                                   ctypes.POINTER(ctypes.c_size_t)]
+    lib.bnn_experts_sum.argtypes = [ctypes.POINTER(ExpertsDesc), P, P, P, P, P, P, P, i32, P, P,
+                                    ctypes.c_size_t, P]
+    lib.bnn_bgemm_lora_workspace_size.argtypes = [ctypes.POINTER(LoraDesc),
+                                                  ctypes.POINTER(ctypes.c_size_t)]
+    lib.bnn_bgemm_lora.argtypes = [ctypes.POINTER(LoraDesc), P, i64, P, P, P, P, P, P, P, P, P, P,
+                                   ctypes.c_size_t, P]
     lib.bnn_forward_workspace_size.argtypes = [ctypes.POINTER(Layer), i32, i32, i32, i32, i32,
                                                ctypes.POINTER(ctypes.c_size_t)]
     lib.bnn_forward.argtypes = [ctypes.POINTER(Layer), i32, i32, i32, i32, i32, P, P,
@@ -519,6 +548,189 @@ def bnn_bgemm(A, B, K, thr=None, flip=None, want_sums=True, want_bits=True, out_
     return out_sums, out_bits
 
 
+# ---------------------------------------------- mixtures of binary experts ---
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int32: 3}
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _real(dtype, name):
+    code = _DTYPES.get(dtype)
+    if code is None or code == 3:
+        raise TypeError("%s must be float32, float16 or bfloat16" % name)
+    return code
+
+
+def _shaped(t, shape, name):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return t
+
+
+def _rows(t, name):
+    """A 2-d tensor whose rows are contiguous: their distance in elements."""
+    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a 2-d CUDA(HIP) tensor with contiguous rows" % name)
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def bnn_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=None, group_top=1,
+              renormalize=True, scale=1.0, logit_scale=1.0, ids=None, weights=None, stream=None):
+    """Routing: logits [T, E] (float32, float16, bfloat16 or int32; rows may be
+    strided) -> (ids [T, top_k] int32, weights [T, top_k] float32).  The
+    experts of the largest p + bias (p: softmax or sigmoid of logit_scale *
+    logits), with groups > 1 out of the top_groups groups of the largest
+    scores; weights are scale * p, with renormalize over the chosen experts'
+    sum.  Experts out of reach (logit -inf) are never chosen: id -1."""
+    lib = load()
+    dtype = _DTYPES.get(logits.dtype)
+    if dtype is None:
+        raise TypeError("logits must be float32, float16, bfloat16 or int32")
+    stride = _rows(logits, "logits")
+    T, E = logits.shape
+    bias = _shaped(_dev(bias, torch.float32, "bias"), (E,), "bias")
+    if ids is None:
+        ids = torch.empty((T, top_k), dtype=torch.int32, device=logits.device)
+    if weights is None:
+        weights = torch.empty((T, top_k), dtype=torch.float32, device=logits.device)
+    _shaped(_dev(ids, torch.int32, "ids"), (T, top_k), "ids")
+    _shaped(_dev(weights, torch.float32, "weights"), (T, top_k), "weights")
+    if score not in _SCORES:
+        raise ValueError("score must be one of %s" % sorted(_SCORES))
+    d = RouteDesc(E, top_k, groups, groups if top_groups is None else top_groups, group_top,
+                  _SCORES[score], bool(renormalize), dtype, scale, logit_scale)
+    _check(lib.bnn_route(ctypes.byref(d), T, _ptr(logits), stride, _ptr(bias), _ptr(ids),
+                         _ptr(weights), _stream(stream)))
+    return ids, weights
+
+
+def bnn_group_rows(ids, G, offsets=None, order=None, stream=None):
+    """Rows in the order of their group: ids (any shape, int32) -> (offsets
+    [G + 1], order [ids.numel()]) int32; rows whose id is not in [0, G) come
+    last."""
+    lib = load()
+    _dev(ids, torch.int32, "ids")
+    M = ids.numel()
+    if offsets is None:
+        offsets = torch.empty(G + 1, dtype=torch.int32, device=ids.device)
+    if order is None:
+        order = torch.empty(M, dtype=torch.int32, device=ids.device)
+    _shaped(_dev(offsets, torch.int32, "offsets"), (G + 1,), "offsets")
+    _shaped(_dev(order, torch.int32, "order"), (M,), "order")
+    _check(lib.bnn_group_rows(M, G, _ptr(ids), _ptr(offsets), _ptr(order), _stream(stream)))
+    return offsets, order
+
+
+def _experts_desc(x, K, w, M, top_k, offsets, order):
+    """The description of M = T * top_k pairs over x [T, Kw] or [M, Kw]."""
+    _u32(x)
+    _u32(w)
+    E, N, kw = w.shape
+    T = M // top_k
+    if x.dim() != 2 or x.shape[1] != kw or kw != words(K) or x.shape[0] not in (T, M):
+        raise ValueError("x must be [%d or %d, %d] packed words of %d bits" % (T, M, words(K), K))
+    _shaped(_dev(offsets, torch.int32, "offsets"), (E + 1,), "offsets")
+    _shaped(_dev(order, torch.int32, "order"), (M,), "order")
+    return ExpertsDesc(T, top_k, E, N, K, int(top_k > 1 and x.shape[0] == T))
+
+
+def bnn_experts_fc(x, K, w, offsets, order, thr, flip=None, out_bits=None, stream=None):
+    """Binary FC layers of experts, to bits: x [T, Kw] (a row's experts read
+    the same bits) or [M, Kw], M = order.numel() (row, expert) pairs; w
+    [E, N, Kw], thr [E, N], flip [E, ceil(N/32)]; offsets and order of
+    bnn_group_rows -> bits [M, ceil(N/32)] (0 for a pair without an expert)."""
+    lib = load()
+    M, rows = order.numel(), x.shape[0]
+    if M and (not rows or M % rows):
+        raise ValueError("%d pairs do not go evenly over %d rows of x" % (M, rows))
+    d = _experts_desc(x, K, w, M, M // rows if M else 1, offsets, order)
+    nw = words(d.N)
+    _shaped(_dev(thr, torch.int32, "thr"), (d.E, d.N), "thr")
+    _shaped(_dev(flip, torch.int32, "flip"), (d.E, nw), "flip")
+    if out_bits is None:
+        out_bits = torch.empty((M, nw), dtype=torch.int32, device=x.device)
+    _shaped(_u32(out_bits), (M, nw), "out_bits")
+    _check(lib.bnn_experts_fc(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(offsets), _ptr(order),
+                              _ptr(thr), _ptr(flip), _ptr(out_bits), _stream(stream)))
+    return out_bits
+
+
+def bnn_experts_sum_workspace_size(desc: ExpertsDesc) -> int:
+    out = ctypes.c_size_t()
+    _check(load().bnn_experts_sum_workspace_size(ctypes.byref(desc), ctypes.byref(out)))
+    return out.value
+
+
+def bnn_experts_sum(x, K, w, ids, weights, offsets, order, alpha=None, dtype=torch.float32,
+                    out=None, workspace=None, stream=None):
+    """Binary FC layers of experts, weighted and added up per row: ids and
+    weights [T, top_k] (of bnn_route), x [T * top_k, Kw] or [T, Kw], w
+    [E, N, Kw], alpha [E, N] float32; offsets and order of bnn_group_rows(ids)
+    -> y [T, N] of dtype, y[t] = sum_j weights[t, j] * alpha[e] * S[t, j]."""
+    lib = load()
+    _dev(ids, torch.int32, "ids")
+    T, top_k = ids.shape
+    _shaped(_dev(weights, torch.float32, "weights"), (T, top_k), "weights")
+    d = _experts_desc(x, K, w, T * top_k, top_k, offsets, order)
+    _shaped(_dev(alpha, torch.float32, "alpha"), (d.E, d.N), "alpha")
+    if out is None:
+        out = torch.empty((T, d.N), dtype=dtype, device=x.device)
+    code = _real(out.dtype, "out")
+    _shaped(_dev(out, out.dtype, "out"), (T, d.N), "out")
+    if workspace is None:
+        n = bnn_experts_sum_workspace_size(d)
+        workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+    n = 0 if workspace is None else _dev(workspace, torch.uint8, "workspace").numel()
+    _check(lib.bnn_experts_sum(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(ids), _ptr(weights),
+                               _ptr(offsets), _ptr(order), _ptr(alpha), code, _ptr(out),
+                               _ptr(workspace), n, _stream(stream)))
+    return out
+
+
+def bnn_bgemm_lora_workspace_size(desc: LoraDesc) -> int:
+    out = ctypes.c_size_t()
+    _check(load().bnn_bgemm_lora_workspace_size(ctypes.byref(desc), ctypes.byref(out)))
+    return out.value
+
+
+def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=None, dtype=None,
+                   out=None, workspace=None, stream=None):
+    """A binary FC layer with a low-rank adapter per row: x [M, K] (float32,
+    float16 or bfloat16; rows may be strided), w [N, Kw] packed, ids [M] the
+    rows' adapters (-1: none), a [L, rank, K] and b [L, N, rank] of x's type,
+    scale [L], alpha [N], offset [K] float32 -> y [M, N] of dtype (x's),
+    y = alpha * (sign(x + offset) . w) + scale[l] * (x a[l]^T) b[l]^T.
+    order: bnn_group_rows(ids, L)[1], or None."""
+    lib = load()
+    kind = x.dtype
+    code = _real(kind, "x")
+    stride = _rows(x, "x")
+    M, K = x.shape
+    _u32(w)
+    N = w.shape[0]
+    _shaped(w, (N, words(K)), "w")
+    _dev(a, kind, "a")
+    L, rank = a.shape[0], a.shape[1]
+    _shaped(a, (L, rank, K), "a")
+    _shaped(_dev(b, kind, "b"), (L, N, rank), "b")
+    _shaped(_dev(ids, torch.int32, "ids"), (M,), "ids")
+    _shaped(_dev(order, torch.int32, "order"), (M,), "order")
+    _shaped(_dev(scale, torch.float32, "scale"), (L,), "scale")
+    _shaped(_dev(alpha, torch.float32, "alpha"), (N,), "alpha")
+    _shaped(_dev(offset, torch.float32, "offset"), (K,), "offset")
+    if out is None:
+        out = torch.empty((M, N), dtype=kind if dtype is None else dtype, device=x.device)
+    _shaped(_dev(out, out.dtype, "out"), (M, N), "out")
+    d = LoraDesc(M, N, K, L, rank, code, _real(out.dtype, "out"))
+    if workspace is None:
+        workspace = torch.empty(bnn_bgemm_lora_workspace_size(d), dtype=torch.uint8,
+                                device=x.device)
+    _dev(workspace, torch.uint8, "workspace")
+    _check(lib.bnn_bgemm_lora(ctypes.byref(d), _ptr(x), stride, _ptr(offset), _ptr(w),
+                              _ptr(alpha), _ptr(ids), _ptr(a), _ptr(b), _ptr(scale), _ptr(order),
+                              _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return out
+
+
 class Network:
     """A layer chain for bnn_forward.  ``layers`` holds dicts with the C
     struct's fields and device tensors (w, thr, flip, offset); the tensors are
@@ -593,4 +805,9 @@ bconv2d_input = bnn_bconv2d_input
 fconv_bconv2d = bnn_fconv_bconv2d
 binarize_input = bnn_binarize_input
 bgemm = bnn_bgemm
+route = bnn_route
+group_rows = bnn_group_rows
+experts_fc = bnn_experts_fc
+experts_sum = bnn_experts_sum
+bgemm_lora = bnn_bgemm_lora
 forward = bnn_forward

@@ -13,27 +13,15 @@
 #include <new>
 
 #include "kernels.hpp"
+#include "status.hpp"
 
 namespace {
 
 thread_local char g_err[512] = "";
 
-bnn_options default_options() {
-  bnn_options o;
-  o.algo = BNN_ALGO_AUTO;
-  o.fuse_input = 1;
-  o.fuse_first = 1;
-  o.fc_chain = 1;
-  o.conv1x1 = 1;
-  o.xcd_order = 1;
-  o.gemv_max_rows = 1;
-  o.lds_weights = -1;
-  o.late_thresholds = -1;
-  o.fuse_pair = 1;
-  return o;
-}
+}  // namespace
 
-thread_local bnn_options g_opt = default_options();
+namespace bnn {
 
 bnn_status fail(bnn_status st, const char* fmt, ...) {
   va_list ap;
@@ -52,6 +40,31 @@ bnn_status hip_status(hipError_t e, const char* where) {
   if (e == hipSuccess) return ok();
   return fail(BNN_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
 }
+
+}  // namespace bnn
+
+namespace {
+
+using bnn::fail;
+using bnn::hip_status;
+using bnn::ok;
+
+bnn_options default_options() {
+  bnn_options o;
+  o.algo = BNN_ALGO_AUTO;
+  o.fuse_input = 1;
+  o.fuse_first = 1;
+  o.fc_chain = 1;
+  o.conv1x1 = 1;
+  o.xcd_order = 1;
+  o.gemv_max_rows = 1;
+  o.lds_weights = -1;
+  o.late_thresholds = -1;
+  o.fuse_pair = 1;
+  return o;
+}
+
+thread_local bnn_options g_opt = default_options();
 
 // Kernel family for binary convs / GEMMs: the fp4 matrix-core kernel where
 // the shape allows it, unless the options ask for the XOR-popcount vector

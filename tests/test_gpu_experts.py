@@ -1,0 +1,138 @@
+"""The experts' binary layers against their definition in whole numbers
+(experts_ref): bits word for word; weighted sums within the roundings of their
+top_k products and additions in 32 bits, (top_k + 3) 2^-24 of the magnitudes
+added up (each term: two products and its addition; S is exact), and one
+rounding to the output's type (2^-8 of the value for bf16, 2^-11 for fp16, and
+the smallest fp16 step)."""
+import numpy as np
+import pytest
+import torch
+
+import experts_ref as ref
+from paper_1808_00209_amd import bnn
+
+pytestmark = pytest.mark.gpu
+
+CASES = [
+    # T, top_k, E, K, N, rows without an expert
+    (1, 1, 1, 1, 1, 0.0), (1, 8, 64, 1024, 512, 0.0), (5, 2, 3, 33, 31, 0.2), (7, 3, 4, 64, 64, 0.0),
+    (40, 2, 5, 1000, 130, 0.1), (130, 4, 6, 256, 96, 0.0), (300, 1, 2, 512, 64, 0.3),
+    (64, 8, 16, 2048, 320, 0.0), (3, 16, 40, 95, 33, 0.5), (9, 4, 7, 4100, 100, 0.0),
+    (700, 2, 3, 300, 257, 0.05), (2, 2, 1000, 70, 40, 0.0), (260, 1, 1, 129, 1000, 0.0),
+    (33, 3, 3, 1023, 32, 0.0), (16, 6, 12, 8192, 48, 0.0), (1030, 1, 5, 96, 65, 0.01),
+    (1500, 2, 4, 288, 700, 0.02),
+]
+
+
+def _ids(g, T, k, E, none):
+    """Distinct experts per row where there are enough, popular ones first;
+    one expert in three without any row (of more than two)."""
+    p = 1.0 / (1 + np.arange(E)) ** 1.2
+    if E > 2:
+        p[::3] = 0
+    p /= p.sum()
+    some = np.count_nonzero(p)
+    ids = np.stack([g.choice(E, size=k, replace=k > some, p=p) for _ in range(T)])
+    ids[g.random((T, k)) < none] = -1
+    if none:
+        ids[0] = -1
+        ids[-1, 0] = E  # out of range: no expert either
+    return ids.astype(np.int32)
+
+
+def _words(g, *shape):
+    return g.integers(-2 ** 31, 2 ** 31, size=shape).astype(np.int32)
+
+
+def _dev(*arrays):
+    return [None if a is None else torch.from_numpy(a).cuda() for a in arrays]
+
+
+@pytest.mark.parametrize("per_pair", [False, True])
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_experts_fc(case, per_pair):
+    T, k, E, K, N, none = case
+    g = np.random.default_rng(T + K + N)
+    ids = _ids(g, T, k, E, none)
+    x, w = _words(g, T * k if per_pair else T, bnn.words(K)), _words(g, E, N, bnn.words(K))
+    r = 2 * int(K ** 0.5) + 1
+    thr = g.integers(-r, r + 1, size=(E, N)).astype(np.int32)
+    thr[0, 0], thr[-1, -1] = 2 ** 31 - 1, -2 ** 31
+    for flip in (None, _words(g, E, bnn.words(N))):
+        dx, dw, di, dt, df = _dev(x, w, ids, thr, flip)
+        offsets, order = bnn.bnn_group_rows(di, E)
+        got = bnn.bnn_experts_fc(dx, K, dw, offsets, order, dt, df)
+        torch.cuda.synchronize()
+        assert np.array_equal(got.cpu().numpy(), ref.experts_fc(x, w, ids, K, thr, flip))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_experts_sum(case, dtype):
+    T, k, E, K, N, none = case
+    g = np.random.default_rng(T + K + N + 1)
+    ids = _ids(g, T, k, E, none)
+    for per_pair, scaled in ((True, True), (False, False)):
+        x, w = _words(g, T * k if per_pair else T, bnn.words(K)), _words(g, E, N, bnn.words(K))
+        weights = g.random((T, k)).astype(np.float32) - 0.25
+        weights[ids < 0] = np.nan  # is not read
+        alpha = (g.standard_normal((E, N)) / np.sqrt(K)).astype(np.float32) if scaled else None
+        dx, dw, di, dv, da = _dev(x, w, ids, weights, alpha)
+        offsets, order = bnn.bnn_group_rows(di, E)
+        got = bnn.bnn_experts_sum(dx, K, dw, di, dv, offsets, order, da, dtype=dtype)
+        torch.cuda.synchronize()
+        want, mag = ref.experts_sum(x, w, ids, weights, K, alpha)
+        got = got.double().cpu().numpy()
+        step = {torch.float32: 0.0, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+        bound = (k + 3) * 2.0 ** -24 * mag
+        bound += step * (np.abs(want) + bound) + (2.0 ** -25 if dtype == torch.float16 else 0)
+        if dtype == torch.float16:
+            over = np.abs(want) > 65000
+            assert not over.any() or not scaled
+            got, want = np.where(over, 0, got), np.where(over, 0, want)
+        assert (np.abs(got - want) <= bound).all()
+
+
+def test_the_same_call_twice_gives_the_same_bits_and_a_stream_of_its_own_too():
+    g = np.random.default_rng(3)
+    T, k, E, K, N = 257, 4, 9, 700, 200
+    ids = _ids(g, T, k, E, 0.1)
+    x, w, weights = _words(g, T, bnn.words(K)), _words(g, E, N, bnn.words(K)), g.random((T, k)).astype(np.float32)
+    dx, dw, di, dv = _dev(x, w, ids, weights)
+    offsets, order = bnn.bnn_group_rows(di, E)
+    first = bnn.bnn_experts_sum(dx, K, dw, di, dv, offsets, order)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = torch.empty_like(first)
+    with torch.cuda.stream(s):
+        o2 = bnn.bnn_group_rows(di, E)
+        bnn.bnn_experts_sum(dx, K, dw, di, dv, *o2, out=out)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    assert torch.equal(first, out)
+
+
+def test_no_rows_and_shapes_that_disagree():
+    w = torch.zeros((3, 40, 2), dtype=torch.int32, device="cuda")
+    ids = torch.zeros((0, 2), dtype=torch.int32, device="cuda")
+    offsets, order = bnn.bnn_group_rows(ids, 3)
+    assert offsets.tolist() == [0, 0, 0, 0]
+    thr = torch.zeros((3, 40), dtype=torch.int32, device="cuda")
+    x = torch.zeros((0, 2), dtype=torch.int32, device="cuda")
+    assert bnn.bnn_experts_fc(x, 64, w, offsets, order, thr).shape == (0, 2)
+    y = bnn.bnn_experts_sum(x, 64, w, ids, torch.zeros((0, 2), device="cuda"), offsets, order)
+    assert y.shape == (0, 40)
+    ids = torch.zeros((4, 2), dtype=torch.int32, device="cuda")
+    offsets, order = bnn.bnn_group_rows(ids, 3)
+    for rows in (3, 5):
+        with pytest.raises(ValueError):
+            bnn.bnn_experts_fc(torch.zeros((rows, 2), dtype=torch.int32, device="cuda"), 64, w,
+                               offsets, order, thr)
+    x = torch.zeros((4, 2), dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        bnn.bnn_experts_fc(x, 65, w, offsets, order, thr)
+    with pytest.raises(ValueError):
+        bnn.bnn_experts_fc(x, 64, w, offsets, order, thr[:2].contiguous())
+    with pytest.raises(TypeError):
+        bnn.bnn_experts_sum(x, 64, w, ids, torch.zeros((4, 2), device="cuda"), offsets, order,
+                            dtype=torch.float64)

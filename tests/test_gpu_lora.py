@@ -1,0 +1,160 @@
+"""The shared binary layer with adapters per row against its definition in 64
+bits (experts_ref).
+
+Tolerance.  alpha S: S is exact, one product and one addition (2 2^-24 of
+|alpha S|).  The adapter's term: K products and additions in 32 bits for u
+(any order), the factor scale, rank products and additions for the output, and
+u in parts that hold at least 24 bits: (K + rank + 8) 2^-24 of the magnitudes
+added up.  Then one rounding to the output's type: 2^-8 of the value for bf16,
+2^-11 for fp16 (2^-25 at least), 2^-24 for fp32."""
+import numpy as np
+import pytest
+import torch
+
+import experts_ref as ref
+from paper_1808_00209_amd import bnn
+
+pytestmark = pytest.mark.gpu
+
+T = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+CASES = [
+    # M, K, N, adapters, rank, type, out
+    (1, 1, 1, 1, 8, "fp32", "fp32"), (1, 4096, 512, 3, 16, "bf16", "bf16"),
+    (2, 33, 31, 2, 8, "fp16", "fp32"), (7, 1000, 130, 4, 24, "bf16", "fp32"),
+    (16, 64, 64, 1, 64, "fp16", "fp16"), (31, 513, 257, 16, 8, "bf16", "fp16"),
+    (32, 1024, 320, 64, 16, "bf16", "bf16"), (33, 2048, 96, 5, 32, "fp32", "bf16"),
+    (64, 100, 1000, 2, 256, "bf16", "bf16"), (100, 1101, 205, 7, 40, "fp32", "fp32"),
+    (129, 512, 128, 3, 128, "fp16", "bf16"), (300, 777, 65, 9, 8, "fp16", "fp32"),
+    (515, 256, 513, 30, 16, "bf16", "fp32"), (1200, 192, 300, 4, 64, "fp32", "fp32"),
+    (260, 4100, 40, 2, 16, "bf16", "bf16"), (2050, 72, 70, 1000, 8, "bf16", "fp16"),
+]
+
+
+def _inputs(g, M, K, N, L, rank, kind):
+    t = lambda v: torch.from_numpy(v).to(T[kind])  # noqa: E731
+    ids = g.integers(0, L, size=M)
+    ids[g.random(M) < 0.2] = -1
+    if M > 3:
+        ids[1] = L  # out of range: no adapter
+    return dict(x=t(g.standard_normal((M, K))), ids=ids.astype(np.int32),
+                w=g.integers(-2 ** 31, 2 ** 31, size=(N, bnn.words(K))).astype(np.int32),
+                a=t(g.standard_normal((L, rank, K)) / np.sqrt(K)),
+                b=t(g.standard_normal((L, N, rank)) / 2),
+                scale=(0.5 + g.random(L)).astype(np.float32),
+                alpha=(g.standard_normal(N) / np.sqrt(K)).astype(np.float32),
+                offset=(0.1 * g.standard_normal(K)).astype(np.float32))
+
+
+def _reference(p, plain=False):
+    f = lambda v: v.double().numpy() if isinstance(v, torch.Tensor) else v  # noqa: E731
+    opt = {} if plain else {n: f(p[n]) for n in ("scale", "alpha", "offset")}
+    return ref.lora(f(p["x"]), p["w"], p["ids"], f(p["a"]), f(p["b"]), **opt)
+
+
+def _call(p, plain=False, order=None, x=None, **kw):
+    d = lambda v: (v if isinstance(v, torch.Tensor) else torch.from_numpy(v)).cuda()  # noqa: E731
+    opt = {} if plain else {n: d(p[n]) for n in ("scale", "alpha", "offset")}
+    y = bnn.bnn_bgemm_lora(d(p["x"]) if x is None else x, d(p["w"]), d(p["ids"]), d(p["a"]),
+                           d(p["b"]), order=order, **opt, **kw)
+    torch.cuda.synchronize()
+    return y
+
+
+def _assert_near(y, want, K, rank, out):
+    total, base, mag = want
+    bound = 2 * 2.0 ** -24 * base + (K + rank + 8) * 2.0 ** -24 * mag
+    step = {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}[out]
+    bound = bound + step * (np.abs(total) + bound) + (2.0 ** -25 if out == "fp16" else 0.0)
+    got = y.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    assert (np.abs(got - total) <= bound).all(), np.abs(got - total).max()
+
+
+@pytest.mark.parametrize("grouped", ["mixed", "ordered", "runs"])
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_lora(case, grouped):
+    M, K, N, L, rank, kind, out = case
+    g = np.random.default_rng(M + K + N)
+    p = _inputs(g, M, K, N, L, rank, kind)
+    if grouped == "runs":
+        p["ids"] = np.sort(p["ids"])
+    order = None
+    if grouped == "ordered":
+        order = bnn.bnn_group_rows(torch.from_numpy(p["ids"]).cuda(), L)[1]
+    y = _call(p, order=order, dtype=T[out])
+    assert y.dtype == T[out]
+    _assert_near(y, _reference(p), K, rank, out)
+    if grouped == "mixed":
+        y = _call(p, plain=True, dtype=T[out])
+        want = _reference(p, plain=True)
+        if out != "fp16" or np.abs(want[0]).max() < 60000:
+            _assert_near(y, want, K, rank, out)
+
+
+def test_rows_without_an_adapter_are_the_binary_layer():
+    g = np.random.default_rng(9)
+    p = _inputs(g, 70, 1024, 96, 2, 8, "fp32")
+    p["ids"][:] = -1
+    y = _call(p, plain=True)
+    sums, _ = bnn.bnn_bgemm(bnn.bnn_pack_bits(p["x"].cuda()), torch.from_numpy(p["w"]).cuda(), 1024,
+                            want_bits=False)
+    assert torch.equal(y, sums.float())
+
+
+def test_zeros_and_ties_of_the_offset_read_minus_one():
+    """x + offset == 0 is bit 0 (-1), as in bnn_pack_bits; the smallest
+    subnormal above it is +1."""
+    K, N = 64, 32
+    x = torch.zeros(3, K)
+    offset = np.zeros(K, np.float32)
+    x[1] = 1.5
+    offset[:32] = -1.5
+    x[2] = 2.0 ** -149
+    offset[32:] = 0.0
+    w = np.full((N, 2), -1, np.int32)  # all +1
+    p = dict(x=x, ids=np.full(3, -1, np.int32), w=w, a=torch.zeros(1, 8, K), b=torch.zeros(1, N, 8),
+             scale=np.ones(1, np.float32), alpha=np.ones(N, np.float32), offset=offset)
+    y = _call(p)
+    assert y[0].tolist() == [-64.0] * N
+    assert y[1].tolist() == [0.0] * N
+    assert y[2].tolist() == [0.0] * N
+
+
+def test_strided_rows():
+    g = np.random.default_rng(11)
+    for kind, K, extra in (("bf16", 512, 64), ("bf16", 510, 3), ("fp32", 300, 5), ("fp16", 96, 1)):
+        p = _inputs(g, 50, K, 70, 3, 16, kind)
+        wide = torch.full((50, K + extra), 7.0, dtype=T[kind], device="cuda")
+        wide[:, :K] = p["x"].cuda()
+        assert torch.equal(_call(p, x=wide[:, :K]), _call(p))
+
+
+def test_a_row_that_is_not_finite_does_not_touch_the_others():
+    g = np.random.default_rng(12)
+    for M in (3, 40, 300):
+        p = _inputs(g, M, 512, 128, 4, 16, "bf16")
+        y = _call(p)
+        p["x"][M // 2, 17] = float("nan")
+        p["x"][0, 3] = float("inf")
+        z = _call(p)
+        keep = [m for m in range(M) if m not in (0, M // 2)]
+        assert torch.equal(y[keep], z[keep])
+
+
+def test_order_and_repetition_do_not_change_a_bit_of_a_row():
+    """A row's sums are taken in an order that does not hang on the rows beside
+    it: with and without `order`, and twice, the bits are the same."""
+    g = np.random.default_rng(13)
+    p = _inputs(g, 200, 700, 96, 6, 8, "bf16")
+    y = _call(p, dtype=torch.float32)
+    assert torch.equal(y, _call(p, dtype=torch.float32))
+    order = bnn.bnn_group_rows(torch.from_numpy(p["ids"]).cuda(), 6)[1]
+    assert torch.equal(y, _call(p, dtype=torch.float32, order=order))
+
+
+def test_no_rows():
+    y = bnn.bnn_bgemm_lora(torch.empty(0, 64, device="cuda"),
+                           torch.zeros((8, 2), dtype=torch.int32, device="cuda"),
+                           torch.zeros(0, dtype=torch.int32, device="cuda"),
+                           torch.zeros(1, 8, 64, device="cuda"), torch.zeros(1, 8, 8, device="cuda"))
+    assert y.shape == (0, 8)
