@@ -1,5 +1,7 @@
-// Binary FC layers of experts (bnn_experts_fc, bnn_experts_sum) on the vector
-// ALU: a thread per output, XOR + popcount over the row's words (Eq. 4).
+// Binary FC layers of experts (bnn_experts_fc, bnn_experts_sum): the choice of
+// kernel, the vector-ALU kernels (a thread per output, XOR + popcount over the
+// row's words, Eq. 4; option algo = BNN_ALGO_VALU and rows of over 4 GiB), and
+// the weighted sum of the matrix-core kernel's counts.
 #include "dtypes.hpp"
 #include "experts.hpp"
 #include "kernels.hpp"
@@ -69,17 +71,88 @@ __global__ __launch_bounds__(kNT) void experts_sum_valu_kernel(ExpertsArgs a) {
   static_cast<Y*>(a.y)[static_cast<size_t>(t) * a.N + n] = from_f32<Y>(y);
 }
 
+// y[t][n] from the counts c = (S + K) / 2 of the row's pairs, 8 outputs per
+// thread: block (row, 8 * kNT outputs).  WIDE: N is a multiple of 8.
+template <class Y, bool WIDE>
+__global__ __launch_bounds__(kNT) void experts_combine_kernel(ExpertsArgs a,
+                                                              const uint16_t* __restrict__ counts) {
+  const int t = blockIdx.x;
+  const int n = 8 * (blockIdx.y * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x));
+  if (n >= a.N) return;
+  float y[8] = {};
+  for (int j = 0; j < a.top_k; ++j) {
+    const int m = t * a.top_k + j;
+    const int e = a.ids[m];
+    if (e < 0 || e >= a.E) continue;
+    const float wt = a.weights[m];
+    const uint16_t* src = counts + static_cast<size_t>(m) * a.N + n;
+    const float* al = a.alpha ? a.alpha + static_cast<size_t>(e) * a.N + n : nullptr;
+    uint16_t c[8];
+    float f[8];
+    if constexpr (WIDE) {
+      const uint4 v = *reinterpret_cast<const uint4*>(src);
+      __builtin_memcpy(c, &v, 16);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = al ? al[i] : 1.0f;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool in = n + i < a.N;
+        c[i] = in ? src[i] : 0;
+        f[i] = in && al ? al[i] : 1.0f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] += wt * f[i] * static_cast<float>(2 * c[i] - a.K);
+  }
+  Y* dst = static_cast<Y*>(a.y) + static_cast<size_t>(t) * a.N + n;
+  if constexpr (WIDE) {
+    Y out[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = from_f32<Y>(y[i]);
+    __builtin_memcpy(__builtin_assume_aligned(dst, 16), out, sizeof(out));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (n + i < a.N) dst[i] = from_f32<Y>(y[i]);
+  }
+}
+
+bool use_tiles(const ExpertsArgs& a) {
+  return options().algo != BNN_ALGO_VALU && experts_tile_supported(a);
+}
+
 }  // namespace
 
 hipError_t launch_experts_fc(const ExpertsArgs& a, hipStream_t s) {
+  if (use_tiles(a)) return launch_experts_tile(a, nullptr, s);
   const dim3 grid(static_cast<unsigned>(a.M), static_cast<unsigned>((a.N + kNT - 1) / kNT));
   experts_fc_valu_kernel<<<grid, kNT, 0, s>>>(a);
   return hipGetLastError();
 }
 
-size_t experts_sum_workspace(const bnn_experts_desc&) { return 0; }
+// The counts of every pair.
+size_t experts_sum_workspace(const bnn_experts_desc& d) {
+  return static_cast<size_t>(d.T) * d.top_k * d.N * sizeof(uint16_t);
+}
 
 hipError_t launch_experts_sum(const ExpertsArgs& a, hipStream_t s) {
+  if (use_tiles(a)) {
+    uint16_t* counts = static_cast<uint16_t*>(a.ws);
+    const hipError_t err = launch_experts_tile(a, counts, s);
+    if (err != hipSuccess) return err;
+    const int threads = a.N >= 8 * kNT ? kNT : ((a.N + 7) / 8 + 63) / 64 * 64;
+    const dim3 grid(static_cast<unsigned>(a.T),
+                    static_cast<unsigned>((a.N + 8 * threads - 1) / (8 * threads)));
+    with_real_type(a.dtype, [&](auto v) {
+      using Y = decltype(v);
+      if (a.N % 8 == 0)
+        experts_combine_kernel<Y, true><<<grid, threads, 0, s>>>(a, counts);
+      else
+        experts_combine_kernel<Y, false><<<grid, threads, 0, s>>>(a, counts);
+    });
+    return hipGetLastError();
+  }
   const dim3 grid(static_cast<unsigned>(a.T), static_cast<unsigned>((a.N + kNT - 1) / kNT));
   with_real_type(a.dtype, [&](auto v) {
     experts_sum_valu_kernel<decltype(v)><<<grid, kNT, 0, s>>>(a);

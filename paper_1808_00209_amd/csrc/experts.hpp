@@ -37,6 +37,11 @@ struct ExpertsArgs {
 
 hipError_t launch_experts_fc(const ExpertsArgs& a, hipStream_t s);
 
+// The experts' products on the matrix cores (experts_tile.hip): bits, or with
+// counts [M][N] the numbers of equal bits (S + K) / 2.  x of at most 4 GiB.
+bool experts_tile_supported(const ExpertsArgs& a);
+hipError_t launch_experts_tile(const ExpertsArgs& a, uint16_t* counts, hipStream_t s);
+
 size_t experts_sum_workspace(const bnn_experts_desc& d);
 hipError_t launch_experts_sum(const ExpertsArgs& a, hipStream_t s);
 
