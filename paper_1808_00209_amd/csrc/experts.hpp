@@ -65,4 +65,9 @@ struct LoraArgs {
 size_t lora_workspace(const bnn_lora_desc& d);
 hipError_t launch_bgemm_lora(const LoraArgs& a, hipStream_t s);
 
+// The same on the matrix cores (lora_tile.hip); sign bits of at most 4 GiB.
+size_t lora_tile_workspace(int64_t M, int32_t K, int32_t rank);
+bool lora_tile_supported(const LoraArgs& a);
+hipError_t launch_lora_tile(const LoraArgs& a, hipStream_t s);
+
 }  // namespace bnn
