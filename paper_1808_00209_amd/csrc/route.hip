@@ -1,10 +1,21 @@
 // Routing of rows to experts: scores, a balancing bias, groups, the top_k
 // largest keys and their weights (bnn_route).
 //
-// A row's E logits lie in the registers of a wave, expert e in register e / 64
-// of lane e % 64.  Keys are compared with their expert's index, so that
-// equal ones go to the lowest index whatever the lanes' order.
+// A row's E logits lie in the registers of LP lanes, VPL consecutive experts
+// in each.  A key and its expert's index become one 64-bit number whose order
+// is that of the keys, equal keys lowest index first: the mantissa of a double
+// in [1, 2) holds the key's 32 bits made monotone and, below them, the index
+// from the top, so that one v_max_f64 compares both.  Every lane keeps its
+// three largest; a round takes the largest of the row's heads (DPP steps
+// within 16 lanes), and its lane moves up.  A lane that gave three looks
+// through its experts again, which few rows need.  The weights are computed
+// again for the chosen experts alone.
+//
+// 65521 rows of 256 experts in 8 groups, sigmoid scores and a bias: 67 MB of
+// logits, 13 us at 5.1 TB/s; a wave per row with shuffles took 139 us.
 #include <float.h>
+
+#include <type_traits>
 
 #include "dtypes.hpp"
 #include "experts.hpp"
@@ -25,127 +36,263 @@ struct RouteArgs {
   float scale, logit_scale;
 };
 
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  const int v = __float_as_int(x);
+  return __int_as_float(__builtin_amdgcn_update_dpp(v, v, CTRL, 0xF, 0xF, false));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp(double x) {
+  const int lo = __double2loint(x), hi = __double2hiint(x);
+  return __hiloint2double(__builtin_amdgcn_update_dpp(hi, hi, CTRL, 0xF, 0xF, false),
+                          __builtin_amdgcn_update_dpp(lo, lo, CTRL, 0xF, 0xF, false));
+}
+
+// f over the LP lanes of a row; every lane gets the result.  f commutes, so
+// all lanes get the same bits.
+template <int LP, class V, class F>
+__device__ __forceinline__ V row_reduce(V x, F f) {
+  x = f(x, dpp<0xB1>(x));   // quad_perm [1,0,3,2]
+  x = f(x, dpp<0x4E>(x));   // quad_perm [2,3,0,1]
+  x = f(x, dpp<0x141>(x));  // row_half_mirror: the other quad of 8 lanes
+  x = f(x, dpp<0x140>(x));  // row_mirror: the other 8 of 16
+#pragma unroll
+  for (int s = 16; s < LP; s *= 2) x = f(x, __shfl_xor(x, s));
+  return x;
+}
+
+// exp(z) within a few units of the last place: exp2 of the rounded z log2(e)
+// times 1 + the rest; 0 and infinity outside the normal range.
+__device__ __forceinline__ float exp_of(float z) {
+  constexpr float kL = 1.44269502162933349609375f;      // log2(e) rounded
+  constexpr float kLlo = 1.925963033500011079e-8f;      // log2(e) - kL
+  constexpr float kLn2 = 0.693147180559945309417f;
+  z = fminf(fmaxf(z, -1000.0f), 1000.0f);
+  const float t = z * kL;
+  const float rest = fmaf(z, kLlo, fmaf(z, kL, -t));
+  return __builtin_amdgcn_exp2f(t) * fmaf(rest, kLn2, 1.0f);
+}
+
+// A logit as the score's argument; out of reach (-inf and NaN): kNone.
+__device__ __forceinline__ float argument(float raw, float scale) {
+  return raw > kNone ? fminf(fmaxf(raw * scale, -FLT_MAX), FLT_MAX) : kNone;
+}
+
+template <bool SOFTMAX>
+__device__ __forceinline__ float score(float z, float top, float inv_sum) {
+  if constexpr (SOFTMAX) return exp_of(z - top) * inv_sum;
+  return __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
+}
+
+// Key and index as a double in [1, 2); kNone as the key of the index is the
+// smallest of all keys.
+__device__ __forceinline__ double pack_key(float key, int e) {
+  const uint32_t b = __float_as_uint(key);
+  const uint32_t u = b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+  return __hiloint2double(static_cast<int>(__builtin_amdgcn_alignbit(0x3FFu, u, 12)),
+                          static_cast<int>((u << 20) | (0xFFFFFu - static_cast<uint32_t>(e))));
+}
+__device__ __forceinline__ int index_of(double c) {
+  return static_cast<int>(0xFFFFFu - (static_cast<uint32_t>(__double2loint(c)) & 0xFFFFFu));
+}
+constexpr uint32_t kNoneBits = 0x007FFFFFu;  // kNone made monotone
+__device__ __forceinline__ bool reachable(double c) {
+  const uint32_t u = __builtin_amdgcn_alignbit(static_cast<uint32_t>(__double2hiint(c)),
+                                               static_cast<uint32_t>(__double2loint(c)), 20);
+  return u > kNoneBits;
+}
+
+// (The library's fmax and fmin quiet signalling NaNs first, an instruction for
+// each operand; there are none here.)
+__device__ __forceinline__ double max_f64(double x, double y) {
+  double d;
+  asm("v_max_f64 %0, %1, %2" : "=v"(d) : "v"(x), "v"(y));
+  return d;
+}
+__device__ __forceinline__ double min_f64(double x, double y) {
+  double d;
+  asm("v_min_f64 %0, %1, %2" : "=v"(d) : "v"(x), "v"(y));
+  return d;
+}
+
 // LP lanes per row, VPL experts per lane.
 template <int LP, int VPL, bool SOFTMAX, class T>
 __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
   constexpr int kRows = kNT / LP;
-  extern __shared__ float lds[];  // groups: [kRows][E] keys, [kRows][groups] scores
+  extern __shared__ __attribute__((aligned(8))) float lds[];  // groups only
   const int ln = threadIdx.x % LP;
   const int row = threadIdx.x / LP;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + row;
   const bool live = t < a.T;
   const T* src = static_cast<const T*>(a.logits) + (live ? t : a.T - 1) * a.stride;
+  const int e0 = ln * VPL;
 
-  float p[VPL], key[VPL];
-  float top = kNone;
+  T raw[VPL];
+  float key[VPL];
+  if (e0 + VPL <= a.E) {
+    __builtin_memcpy(raw, src + e0, sizeof(raw));
 #pragma unroll
-  for (int i = 0; i < VPL; ++i) {
-    const int e = i * LP + ln;
-    const float raw = e < a.E ? to_f32(src[e]) : kNone;
-    // (false for NaN: such a logit is out of reach as well)
-    const float z = raw > kNone ? fminf(fmaxf(raw * a.logit_scale, -FLT_MAX), FLT_MAX) : kNone;
-    p[i] = z;
-    top = fmaxf(top, z);
-  }
-  if constexpr (SOFTMAX) {
-#pragma unroll
-    for (int s = LP / 2; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, LP));
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      key[i] = p[i];
-      p[i] = p[i] > kNone ? expf(p[i] - top) : 0.0f;
-      sum += p[i];
-    }
-#pragma unroll
-    for (int s = LP / 2; s > 0; s >>= 1) sum += __shfl_xor(sum, s, LP);
-    // (sum >= 1 where any expert is in reach)
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) p[i] = sum > 0.0f ? p[i] / sum : 0.0f;
+    for (int i = 0; i < VPL; ++i) key[i] = argument(to_f32(raw[i]), a.logit_scale);
   } else {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      key[i] = p[i];
-      p[i] = 1.0f / (1.0f + expf(-p[i]));
-    }
+    for (int i = 0; i < VPL; ++i)
+      key[i] = e0 + i < a.E ? argument(to_f32(src[e0 + i]), a.logit_scale) : kNone;
   }
+  float top = 0.0f, inv_sum = 1.0f;
+  if constexpr (SOFTMAX) {
+    top = kNone;
 #pragma unroll
-  for (int i = 0; i < VPL; ++i) {
-    const int e = i * LP + ln;
-    const float b = a.bias && e < a.E ? a.bias[e] : 0.0f;
-    const float v = p[i] + b;
-    key[i] = key[i] > kNone && v > kNone ? v : kNone;
+    for (int i = 0; i < VPL; ++i) top = fmaxf(top, key[i]);
+    top = row_reduce<LP>(top, [](float x, float y) { return fmaxf(x, y); });
+    float sum = 0.0f, ex[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      ex[i] = key[i] > kNone ? exp_of(key[i] - top) : 0.0f;
+      sum += ex[i];
+    }
+    sum = row_reduce<LP>(sum, [](float x, float y) { return x + y; });
+    // (sum >= 1 where any expert is in reach)
+    inv_sum = sum > 0.0f ? __builtin_amdgcn_rcpf(sum) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) key[i] = key[i] > kNone ? ex[i] * inv_sum : kNone;
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i)
+      key[i] = key[i] > kNone ? score<false>(key[i], 0.0f, 0.0f) : kNone;
+  }
+  if (a.bias) {
+    float b[VPL];
+    if (e0 + VPL <= a.E) {
+      __builtin_memcpy(b, a.bias + e0, sizeof(b));
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) b[i] = e0 + i < a.E ? a.bias[e0 + i] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      const float v = key[i] + b[i];
+      key[i] = v > kNone ? v : kNone;
+    }
   }
 
   if (a.groups > 1) {
+    // Groups of whole lanes: the two largest keys of every lane meet in LDS;
+    // other groups: all keys.
+    const bool whole = a.per_group % VPL == 0;
+    float2* pairs = reinterpret_cast<float2*>(lds) + row * (LP + 1);
     float* keys = lds + row * a.E;
-    float* scores = lds + kRows * a.E + row * a.groups;
+    float* scores = lds + kRows * (whole ? 2 * (LP + 1) : a.E) + row * 2 * a.groups;
+    float* kept = scores + a.groups;
+    if (whole) {
+      float2 b = {kNone, kNone};
 #pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (i * LP + ln < a.E) keys[i * LP + ln] = key[i];
+      for (int i = 0; i < VPL; ++i) {
+        b.y = fmaxf(b.y, fminf(b.x, key[i]));
+        b.x = fmaxf(b.x, key[i]);
+      }
+      pairs[ln] = b;
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i)
+        if (e0 + i < a.E) keys[e0 + i] = key[i];
+    }
     __syncthreads();
     for (int g = ln; g < a.groups; g += LP) {
       float b0 = kNone, b1 = kNone;
-      for (int j = 0; j < a.per_group; ++j) {
-        const float v = keys[g * a.per_group + j];
-        b1 = fmaxf(b1, fminf(b0, v));
-        b0 = fmaxf(b0, v);
+      if (whole) {
+        const int n = a.per_group / VPL;
+        for (int j = 0; j < n; ++j) {
+          const float2 v = pairs[g * n + j];
+          b1 = fmaxf(fmaxf(b1, v.y), fminf(b0, v.x));
+          b0 = fmaxf(b0, v.x);
+        }
+      } else {
+        for (int j = 0; j < a.per_group; ++j) {
+          const float v = keys[g * a.per_group + j];
+          b1 = fmaxf(b1, fminf(b0, v));
+          b0 = fmaxf(b0, v);
+        }
       }
       scores[g] = a.group_top == 2 && b1 > kNone ? b0 + b1 : b0;
     }
     __syncthreads();
     // A group is kept where fewer than top_groups come before it.
+    for (int g = ln; g < a.groups; g += LP) {
+      const float mine = scores[g];
+      int before = 0;
+      for (int q = 0; q < a.groups; ++q) {
+        const float v = scores[q];
+        before += v > mine || (v == mine && q < g) ? 1 : 0;
+      }
+      kept[g] = before < a.top_groups ? 1.0f : 0.0f;
+    }
+    __syncthreads();
+    int g = e0 / a.per_group, at = e0 - g * a.per_group;
+    float on = g < a.groups ? kept[g] : 0.0f;
+    if (whole) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      const int e = i * LP + ln;
-      if (e < a.E) {
-        const int g = e / a.per_group;
-        const float mine = scores[g];
-        int before = 0;
-        for (int q = 0; q < a.groups; ++q) {
-          const float v = scores[q];
-          before += v > mine || (v == mine && q < g) ? 1 : 0;
+      for (int i = 0; i < VPL; ++i) key[i] = on != 0.0f ? key[i] : kNone;
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        key[i] = on != 0.0f ? key[i] : kNone;
+        if (++at == a.per_group) {
+          at = 0;
+          ++g;
+          on = g < a.groups ? kept[g] : 0.0f;
         }
-        if (before >= a.top_groups) key[i] = kNone;
       }
     }
   }
 
-  // k rounds: the largest key of the row, and the lowest index that has it.
-  float total = 0.0f, my_w = 0.0f;
-  int my_id = -1;
+  // The lane's three largest; those below `under` where it looks again.
+  double c0, c1, c2;
+  auto largest = [&](auto again, double under) {
+    c0 = c1 = c2 = 0.0;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      double v = pack_key(key[i], e0 + i);
+      if constexpr (decltype(again)::value) v = v < under ? v : 0.0;
+      const double v1 = min_f64(v, c0), v2 = min_f64(v1, c1);
+      c0 = max_f64(c0, v);
+      c1 = max_f64(c1, v1);
+      c2 = max_f64(c2, v2);
+    }
+  };
+  largest(std::false_type{}, 2.0);
+  int given = 0, my_id = -1;
+  double last = 2.0;
   for (int j = 0; j < a.k; ++j) {
-    float bk = kNone, bp = 0.0f;
-    int be = a.E;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (key[i] > bk) {
-        bk = key[i];
-        bp = p[i];
-        be = i * LP + ln;
+    if (VPL > 3 && __ballot(given == 3)) {
+      const double k0 = c0, k1 = c1, k2 = c2;
+      largest(std::true_type{}, last);
+      if (given != 3) {
+        c0 = k0;
+        c1 = k1;
+        c2 = k2;
+      } else {
+        given = 0;
       }
-#pragma unroll
-    for (int s = LP / 2; s > 0; s >>= 1) {
-      const float ok = __shfl_xor(bk, s, LP), op = __shfl_xor(bp, s, LP);
-      const int oe = __shfl_xor(be, s, LP);
-      const bool take = ok > bk || (ok == bk && oe < be);
-      bk = take ? ok : bk;
-      bp = take ? op : bp;
-      be = take ? oe : be;
     }
-    total += bp;
-    if (ln == j) {
-      my_id = bk > kNone ? be : -1;
-      my_w = bp;
+    const double best = row_reduce<LP>(c0, max_f64);
+    if (ln == j && reachable(best)) my_id = index_of(best);
+    if (c0 == best) {  // (one lane of the row, or none has any left)
+      last = c0;
+      c0 = c1;
+      c1 = c2;
+      c2 = 0.0;
+      ++given;
     }
-#pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (i * LP + ln == be) key[i] = kNone;
+  }
+  float w = my_id >= 0 ? score<SOFTMAX>(argument(to_f32(src[my_id]), a.logit_scale), top, inv_sum)
+                       : 0.0f;
+  if (a.renorm) {
+    const float total = row_reduce<LP>(w, [](float x, float y) { return x + y; });
+    w = total > 0.0f ? w / total : 0.0f;
   }
   if (live && ln < a.k) {
-    if (a.renorm) my_w = total > 0.0f ? my_w / total : 0.0f;
     a.ids[t * a.k + ln] = my_id;
-    a.weights[t * a.k + ln] = my_w * a.scale;
+    a.weights[t * a.k + ln] = w * a.scale;
   }
 }
 
@@ -153,7 +300,8 @@ template <int LP, int VPL, class T>
 void launch_shape(const RouteArgs& a, bool softmax, hipStream_t s) {
   constexpr int kRows = kNT / LP;
   const unsigned blocks = static_cast<unsigned>((a.T + kRows - 1) / kRows);
-  const size_t lds = a.groups > 1 ? size_t{kRows} * (a.E + a.groups) * sizeof(float) : 0;
+  const int keys = a.per_group % VPL == 0 ? 2 * (LP + 1) : a.E;
+  const size_t lds = a.groups > 1 ? size_t{kRows} * (keys + 2 * a.groups) * sizeof(float) : 0;
   if (softmax)
     route_kernel<LP, VPL, true, T><<<blocks, kNT, lds, s>>>(a);
   else
@@ -163,9 +311,11 @@ void launch_shape(const RouteArgs& a, bool softmax, hipStream_t s) {
 template <class T>
 void launch_typed(const RouteArgs& a, bool softmax, hipStream_t s) {
   if (a.E <= 64)
-    launch_shape<64, 1, T>(a, softmax, s);
+    launch_shape<16, 4, T>(a, softmax, s);
+  else if (a.E <= 128)
+    launch_shape<16, 8, T>(a, softmax, s);
   else if (a.E <= 256)
-    launch_shape<64, 4, T>(a, softmax, s);
+    launch_shape<16, 16, T>(a, softmax, s);
   else
     launch_shape<64, 16, T>(a, softmax, s);
 }
