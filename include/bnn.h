@@ -543,11 +543,17 @@ bnn_status bnn_route(const bnn_route_desc* d, int64_t T, const void* logits,
  *   order    [M] int32: the rows of group g at offsets[g] .. offsets[g + 1]
  *            - 1 in ascending order, then from offsets[G] on the rows of no
  *            group, in ascending order.
+ *   workspace (device, 16-byte aligned, ws_bytes >= the size that
+ *            bnn_group_rows_workspace_size gives, which is 0 for few rows;
+ *            needs no initialization).
  * 1 <= G <= BNN_MAX_EXPERTS, 0 <= M < 2^24 (M == 0 writes the offsets only).
- * Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_HIP.
+ * Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_WORKSPACE, BNN_ERR_ALIGN (the
+ * workspace), BNN_ERR_HIP.
  */
+bnn_status bnn_group_rows_workspace_size(int64_t M, int32_t G, size_t* bytes);
 bnn_status bnn_group_rows(int64_t M, int32_t G, const int32_t* ids,
-                          int32_t* offsets, int32_t* order, hipStream_t stream);
+                          int32_t* offsets, int32_t* order, void* workspace,
+                          size_t ws_bytes, hipStream_t stream);
 
 typedef struct bnn_experts_desc {
   int64_t T;         /* rows (tokens)                                        */

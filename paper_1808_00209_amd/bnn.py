@@ -39,7 +39,7 @@ EXPORTED = ["bnn_last_error", "bnn_abi_version", "bnn_default_options", "bnn_set
             "bnn_bconv2d_prepared", "bnn_fconv2d_binw", "bnn_binarize_input", "bnn_bconv2d_input",
             "bnn_fconv_bconv2d", "bnn_input_bconv_bconv2d", "bnn_bconv_bconv2d", "bnn_bfc_pair", "bnn_bfc_tail",
             "bnn_bgemm",
-            "bnn_route", "bnn_group_rows", "bnn_experts_fc", "bnn_experts_sum_workspace_size",
+            "bnn_route", "bnn_group_rows_workspace_size", "bnn_group_rows", "bnn_experts_fc", "bnn_experts_sum_workspace_size",
             "bnn_experts_sum", "bnn_bgemm_lora_workspace_size", "bnn_bgemm_lora",
             "bnn_forward_workspace_size", "bnn_forward", "bnn_forward_noalloc"]
 
@@ -136,7 +136,8 @@ def load(path: str = LIB_PATH):
     lib.bnn_bfc_pair.argtypes = [i64, i64, i64, i64, P, P, P, P, P, P, P, P, P, P]
     lib.bnn_bfc_tail.argtypes = [i64, i64, i64, i64, P, P, P, P, P, P, P, P, P, P, P]
     lib.bnn_route.argtypes = [ctypes.POINTER(RouteDesc), i64, P, i64, P, P, P, P]
-    lib.bnn_group_rows.argtypes = [i64, i32, P, P, P, P]
+    lib.bnn_group_rows_workspace_size.argtypes = [i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.bnn_group_rows.argtypes = [i64, i32, P, P, P, P, ctypes.c_size_t, P]
     lib.bnn_experts_fc.argtypes = [ctypes.POINTER(ExpertsDesc), P, P, P, P, P, P, P, P]
     lib.bnn_experts_sum_workspace_size.argtypes = [ctypes.POINTER(ExpertsDesc),
                                                    ctypes.POINTER(ctypes.c_size_t)]
@@ -573,6 +574,13 @@ def _rows(t, name):
     return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
 
 
+def _workspace(ws, need, device):
+    """The caller's workspace, or a new one of `need` bytes, and its size."""
+    if ws is None:
+        return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
+    return ws, _dev(ws, torch.uint8, "workspace").numel()
+
+
 def bnn_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=None, group_top=1,
               renormalize=True, scale=1.0, logit_scale=1.0, ids=None, weights=None, stream=None):
     """Routing: logits [T, E] (float32, float16, bfloat16 or int32; rows may be
@@ -603,7 +611,13 @@ def bnn_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=No
     return ids, weights
 
 
-def bnn_group_rows(ids, G, offsets=None, order=None, stream=None):
+def bnn_group_rows_workspace_size(M, G) -> int:
+    out = ctypes.c_size_t()
+    _check(load().bnn_group_rows_workspace_size(M, G, ctypes.byref(out)))
+    return out.value
+
+
+def bnn_group_rows(ids, G, offsets=None, order=None, workspace=None, stream=None):
     """Rows in the order of their group: ids (any shape, int32) -> (offsets
     [G + 1], order [ids.numel()]) int32; rows whose id is not in [0, G) come
     last."""
@@ -616,7 +630,9 @@ def bnn_group_rows(ids, G, offsets=None, order=None, stream=None):
         order = torch.empty(M, dtype=torch.int32, device=ids.device)
     _shaped(_dev(offsets, torch.int32, "offsets"), (G + 1,), "offsets")
     _shaped(_dev(order, torch.int32, "order"), (M,), "order")
-    _check(lib.bnn_group_rows(M, G, _ptr(ids), _ptr(offsets), _ptr(order), _stream(stream)))
+    workspace, n = _workspace(workspace, bnn_group_rows_workspace_size(M, G), ids.device)
+    _check(lib.bnn_group_rows(M, G, _ptr(ids), _ptr(offsets), _ptr(order), _ptr(workspace), n,
+                              _stream(stream)))
     return offsets, order
 
 
@@ -676,10 +692,7 @@ def bnn_experts_sum(x, K, w, ids, weights, offsets, order, alpha=None, dtype=tor
         out = torch.empty((T, d.N), dtype=dtype, device=x.device)
     code = _real(out.dtype, "out")
     _shaped(_dev(out, out.dtype, "out"), (T, d.N), "out")
-    if workspace is None:
-        n = bnn_experts_sum_workspace_size(d)
-        workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
-    n = 0 if workspace is None else _dev(workspace, torch.uint8, "workspace").numel()
+    workspace, n = _workspace(workspace, bnn_experts_sum_workspace_size(d), x.device)
     _check(lib.bnn_experts_sum(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(ids), _ptr(weights),
                                _ptr(offsets), _ptr(order), _ptr(alpha), code, _ptr(out),
                                _ptr(workspace), n, _stream(stream)))
@@ -721,13 +734,10 @@ def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=N
         out = torch.empty((M, N), dtype=kind if dtype is None else dtype, device=x.device)
     _shaped(_dev(out, out.dtype, "out"), (M, N), "out")
     d = LoraDesc(M, N, K, L, rank, code, _real(out.dtype, "out"))
-    if workspace is None:
-        workspace = torch.empty(bnn_bgemm_lora_workspace_size(d), dtype=torch.uint8,
-                                device=x.device)
-    _dev(workspace, torch.uint8, "workspace")
+    workspace, n = _workspace(workspace, bnn_bgemm_lora_workspace_size(d), x.device)
     _check(lib.bnn_bgemm_lora(ctypes.byref(d), _ptr(x), stride, _ptr(offset), _ptr(w),
                               _ptr(alpha), _ptr(ids), _ptr(a), _ptr(b), _ptr(scale), _ptr(order),
-                              _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream)))
+                              _ptr(out), _ptr(workspace), n, _stream(stream)))
     return out
 
 

@@ -13,8 +13,9 @@ namespace bnn {
 hipError_t launch_route(const bnn_route_desc& d, int64_t T, const void* logits, int64_t stride,
                         const float* bias, int32_t* ids, float* weights, hipStream_t s);
 
+size_t group_rows_workspace(int64_t M, int32_t G);
 hipError_t launch_group_rows(int64_t M, int32_t G, const int32_t* ids, int32_t* offsets,
-                             int32_t* order, hipStream_t s);
+                             int32_t* order, void* ws, hipStream_t s);
 
 struct ExpertsArgs {
   const uint32_t* x;       // [T or M][Kw]

@@ -47,6 +47,20 @@ bnn_status route_check(const bnn_route_desc* d, int64_t T, int64_t stride) {
   return BNN_OK;
 }
 
+bnn_status group_check(int64_t M, int32_t G) {
+  if (M < 0 || M >= kMaxRows || G < 1 || G > BNN_MAX_EXPERTS)
+    return fail(BNN_ERR_SHAPE, "group_rows: M=%lld rows, %d groups", (long long)M, G);
+  return BNN_OK;
+}
+
+bnn_status workspace_check(const char* what, const void* ws, size_t bytes, size_t need) {
+  if (bytes < need || (need && !ws))
+    return fail(BNN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, bytes, need);
+  if (need && !aligned16(ws))
+    return fail(BNN_ERR_ALIGN, "%s: the workspace must be 16-byte aligned", what);
+  return BNN_OK;
+}
+
 bnn_status experts_check(const bnn_experts_desc* d, const char* what) {
   if (!d) return fail(BNN_ERR_NULL, "%s: descriptor is NULL", what);
   if (d->E < 1 || d->E > BNN_MAX_EXPERTS)
@@ -117,14 +131,29 @@ bnn_status bnn_route(const bnn_route_desc* d, int64_t T, const void* logits, int
   }
 }
 
-bnn_status bnn_group_rows(int64_t M, int32_t G, const int32_t* ids, int32_t* offsets,
-                          int32_t* order, hipStream_t stream) {
+bnn_status bnn_group_rows_workspace_size(int64_t M, int32_t G, size_t* bytes) {
   try {
-    if (M < 0 || M >= kMaxRows || G < 1 || G > BNN_MAX_EXPERTS)
-      return fail(BNN_ERR_SHAPE, "group_rows: M=%lld rows, %d groups", (long long)M, G);
+    const bnn_status st = group_check(M, G);
+    if (st != BNN_OK) return st;
+    if (!bytes) return fail(BNN_ERR_NULL, "group_rows: bytes is NULL");
+    *bytes = bnn::group_rows_workspace(M, G);
+    return ok();
+  } catch (...) {
+    return fail(BNN_ERR_HIP, "group_rows: unexpected C++ exception");
+  }
+}
+
+bnn_status bnn_group_rows(int64_t M, int32_t G, const int32_t* ids, int32_t* offsets,
+                          int32_t* order, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  try {
+    const bnn_status st = group_check(M, G);
+    if (st != BNN_OK) return st;
     if (!offsets || (M > 0 && (!ids || !order)))
       return fail(BNN_ERR_NULL, "group_rows: ids, offsets and order must be non-NULL");
-    return hip_status(bnn::launch_group_rows(M, G, ids, offsets, order, stream),
+    const bnn_status ws = workspace_check("group_rows", workspace, ws_bytes,
+                                          bnn::group_rows_workspace(M, G));
+    if (ws != BNN_OK) return ws;
+    return hip_status(bnn::launch_group_rows(M, G, ids, offsets, order, workspace, stream),
                       "group_rows launch");
   } catch (...) {
     return fail(BNN_ERR_HIP, "group_rows: unexpected C++ exception");
@@ -179,12 +208,9 @@ bnn_status bnn_experts_sum(const bnn_experts_desc* d, const uint32_t* x, const u
                   "experts_sum: x, w, ids, weights, offsets, order and y must be non-NULL");
     if (!aligned16(x) || !aligned16(w) || !aligned16(y))
       return fail(BNN_ERR_ALIGN, "experts_sum: x, w and y must be 16-byte aligned");
-    const size_t need = bnn::experts_sum_workspace(*d);
-    if (ws_bytes < need || (need && !workspace))
-      return fail(BNN_ERR_WORKSPACE, "experts_sum: workspace of %zu bytes, %zu needed", ws_bytes,
-                  need);
-    if (need && !aligned16(workspace))
-      return fail(BNN_ERR_ALIGN, "experts_sum: the workspace must be 16-byte aligned");
+    const bnn_status ws = workspace_check("experts_sum", workspace, ws_bytes,
+                                          bnn::experts_sum_workspace(*d));
+    if (ws != BNN_OK) return ws;
     bnn::ExpertsArgs a = experts_args(*d, x, w, offsets, order);
     a.ids = ids;
     a.weights = weights;
@@ -225,11 +251,8 @@ bnn_status bnn_bgemm_lora(const bnn_lora_desc* d, const void* x, int64_t x_strid
       return fail(BNN_ERR_NULL, "lora: x, w, ids, a, b and y must be non-NULL");
     if (!aligned16(x) || !aligned16(w) || !aligned16(a) || !aligned16(b) || !aligned16(y))
       return fail(BNN_ERR_ALIGN, "lora: x, w, a, b and y must be 16-byte aligned");
-    const size_t need = bnn::lora_workspace(*d);
-    if (ws_bytes < need || !workspace)
-      return fail(BNN_ERR_WORKSPACE, "lora: workspace of %zu bytes, %zu needed", ws_bytes, need);
-    if (!aligned16(workspace))
-      return fail(BNN_ERR_ALIGN, "lora: the workspace must be 16-byte aligned");
+    const bnn_status ws = workspace_check("lora", workspace, ws_bytes, bnn::lora_workspace(*d));
+    if (ws != BNN_OK) return ws;
     bnn::LoraArgs g = {};
     g.x = x;
     g.offset = offset;

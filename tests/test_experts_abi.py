@@ -56,11 +56,24 @@ def test_route_arguments(lib):
 
 
 def test_group_rows_arguments(lib):
-    call = lambda M=4, G=2, i=P, f=P, o=P: lib.bnn_group_rows(M, G, i, f, o, None)  # noqa: E731
+    def call(M=4, G=2, i=P, f=P, o=P, ws=P, n=1 << 40):
+        return lib.bnn_group_rows(M, G, i, f, o, ws, n, None)
+
+    n = ctypes.c_size_t()
     for kw in (dict(M=-1), dict(M=1 << 24), dict(G=0), dict(G=1025)):
         _refused(call(**kw), "BNN_ERR_SHAPE", "group_rows")
+        size = dict(M=4, G=2)
+        size.update(kw)
+        _refused(lib.bnn_group_rows_workspace_size(size["M"], size["G"], ctypes.byref(n)),
+                 "BNN_ERR_SHAPE", "group_rows")
     for kw in (dict(i=None), dict(f=None), dict(o=None), dict(M=0, f=None)):
         _refused(call(**kw), "BNN_ERR_NULL", "group_rows")
+    _refused(lib.bnn_group_rows_workspace_size(4, 2, None), "BNN_ERR_NULL", "bytes")
+    assert bnn.bnn_group_rows_workspace_size(1000, 64) == 0
+    need = bnn.bnn_group_rows_workspace_size(1 << 20, 64)
+    _refused(call(M=1 << 20, G=64, n=need - 1), "BNN_ERR_WORKSPACE", "group_rows")
+    _refused(call(M=1 << 20, G=64, ws=None), "BNN_ERR_WORKSPACE", "group_rows")
+    _refused(call(M=1 << 20, G=64, ws=P + 4), "BNN_ERR_ALIGN", "group_rows")
 
 
 def _experts_desc(**kw):

@@ -136,7 +136,7 @@ def test_strided_rows_and_no_rows():
 
 GROUP_CASES = [(0, 1), (1, 1), (1, 1024), (63, 5), (64, 64), (65, 2), (1000, 256), (1023, 7),
                (1024, 7), (1025, 7), (5000, 1000), (8192, 64), (70001, 33), (262144, 8),
-               (131072, 256), (300000, 300)]
+               (131072, 256), (300000, 300), (16384, 100), (16385, 1023), (20000, 1024), (3000001, 77)]
 
 
 @pytest.mark.parametrize("M, G", GROUP_CASES, ids=str)
