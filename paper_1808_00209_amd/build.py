@@ -22,7 +22,8 @@ BUILD_DIR = os.path.join(PKG, "_build")
 SOURCES = ["pack.hip", "bconv_valu.hip", "bconv_mfma.hip", "bconv_tile.hip", "bconv_1x1.hip",
            "bconv_patch.hip", "fconv.hip", "fconv_bconv.hip", "bconv_bconv.hip", "bfc_chain.hip",
            "bfc_pair.hip", "bfc_gemm.hip", "bfc_tile.hip", "route.hip", "group_rows.hip",
-           "experts.hip", "experts_tile.hip",
+           "experts.hip", "experts_tile.hip", "experts_skinny.hip",
+           "experts_combine.hip",
            "lora.hip", "lora_tile.hip", "api.cpp", "experts_api.cpp"]
 ARCH = os.environ.get("BNN_OFFLOAD_ARCH", "gfx950")
 

@@ -1,7 +1,6 @@
 // Binary FC layers of experts (bnn_experts_fc, bnn_experts_sum): the choice of
 // kernel, the vector-ALU kernels (a thread per output, XOR + popcount over the
-// row's words, Eq. 4; option algo = BNN_ALGO_VALU and rows of over 4 GiB), and
-// the weighted sum of the matrix-core kernel's counts.
+// row's words, Eq. 4; option algo = BNN_ALGO_VALU and rows of over 4 GiB).
 #include "dtypes.hpp"
 #include "experts.hpp"
 #include "kernels.hpp"
@@ -71,61 +70,27 @@ __global__ __launch_bounds__(kNT) void experts_sum_valu_kernel(ExpertsArgs a) {
   static_cast<Y*>(a.y)[static_cast<size_t>(t) * a.N + n] = from_f32<Y>(y);
 }
 
-// y[t][n] from the counts c = (S + K) / 2 of the row's pairs, 8 outputs per
-// thread: block (row, 8 * kNT outputs).  WIDE: N is a multiple of 8.
-template <class Y, bool WIDE>
-__global__ __launch_bounds__(kNT) void experts_combine_kernel(ExpertsArgs a,
-                                                              const uint16_t* __restrict__ counts) {
-  const int t = blockIdx.x;
-  const int n = 8 * (blockIdx.y * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x));
-  if (n >= a.N) return;
-  float y[8] = {};
-  for (int j = 0; j < a.top_k; ++j) {
-    const int m = t * a.top_k + j;
-    const int e = a.ids[m];
-    if (e < 0 || e >= a.E) continue;
-    const float wt = a.weights[m];
-    const uint16_t* src = counts + static_cast<size_t>(m) * a.N + n;
-    const float* al = a.alpha ? a.alpha + static_cast<size_t>(e) * a.N + n : nullptr;
-    uint16_t c[8];
-    float f[8];
-    if constexpr (WIDE) {
-      const uint4 v = *reinterpret_cast<const uint4*>(src);
-      __builtin_memcpy(c, &v, 16);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = al ? al[i] : 1.0f;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bool in = n + i < a.N;
-        c[i] = in ? src[i] : 0;
-        f[i] = in && al ? al[i] : 1.0f;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] += wt * f[i] * static_cast<float>(2 * c[i] - a.K);
-  }
-  Y* dst = static_cast<Y*>(a.y) + static_cast<size_t>(t) * a.N + n;
-  if constexpr (WIDE) {
-    Y out[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = from_f32<Y>(y[i]);
-    __builtin_memcpy(__builtin_assume_aligned(dst, 16), out, sizeof(out));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (n + i < a.N) dst[i] = from_f32<Y>(y[i]);
-  }
-}
-
 bool use_tiles(const ExpertsArgs& a) {
   return options().algo != BNN_ALGO_VALU && experts_tile_supported(a);
+}
+
+// The skinny kernel has a workgroup per 32 rows of an expert and 32 outputs,
+// and splits K over its waves: quicker while the whole chip takes about one
+// round of them, several times slower at many (measured, skinny against tile
+// kernel, rows x experts per row of E, K -> N: 1 x 8 of 64, 1024 -> 4096: 5.7
+// and 6.4 us, 4 x 8: 12.1 and 8.7; 4 x 8, 4096 -> 1024: 8.3 and 10.7, 64 x 8: 19.2
+// and 11.4; 1 of 4, 4096 -> 4096: 4.6 and 10.6; 1000 x 2 of 8, 512 -> 512: 4.5 and
+// 5.7; 301 x 3 of 24, 1000 -> 1500: 10.3 and 6.9).
+hipError_t launch_products(const ExpertsArgs& a, uint16_t* counts, hipStream_t s) {
+  const int64_t tiles = (a.M + 31) / 32 + (a.E < a.M ? a.E : a.M);
+  return tiles * words_of(a.N) <= 1200 ? launch_experts_skinny(a, counts, s)
+                                       : launch_experts_tile(a, counts, s);
 }
 
 }  // namespace
 
 hipError_t launch_experts_fc(const ExpertsArgs& a, hipStream_t s) {
-  if (use_tiles(a)) return launch_experts_tile(a, nullptr, s);
+  if (use_tiles(a)) return launch_products(a, nullptr, s);
   const dim3 grid(static_cast<unsigned>(a.M), static_cast<unsigned>((a.N + kNT - 1) / kNT));
   experts_fc_valu_kernel<<<grid, kNT, 0, s>>>(a);
   return hipGetLastError();
@@ -139,19 +104,9 @@ size_t experts_sum_workspace(const bnn_experts_desc& d) {
 hipError_t launch_experts_sum(const ExpertsArgs& a, hipStream_t s) {
   if (use_tiles(a)) {
     uint16_t* counts = static_cast<uint16_t*>(a.ws);
-    const hipError_t err = launch_experts_tile(a, counts, s);
+    const hipError_t err = launch_products(a, counts, s);
     if (err != hipSuccess) return err;
-    const int threads = a.N >= 8 * kNT ? kNT : ((a.N + 7) / 8 + 63) / 64 * 64;
-    const dim3 grid(static_cast<unsigned>(a.T),
-                    static_cast<unsigned>((a.N + 8 * threads - 1) / (8 * threads)));
-    with_real_type(a.dtype, [&](auto v) {
-      using Y = decltype(v);
-      if (a.N % 8 == 0)
-        experts_combine_kernel<Y, true><<<grid, threads, 0, s>>>(a, counts);
-      else
-        experts_combine_kernel<Y, false><<<grid, threads, 0, s>>>(a, counts);
-    });
-    return hipGetLastError();
+    return launch_experts_combine(a, counts, s);
   }
   const dim3 grid(static_cast<unsigned>(a.T), static_cast<unsigned>((a.N + kNT - 1) / kNT));
   with_real_type(a.dtype, [&](auto v) {

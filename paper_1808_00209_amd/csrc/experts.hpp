@@ -42,6 +42,10 @@ hipError_t launch_experts_fc(const ExpertsArgs& a, hipStream_t s);
 // counts [M][N] the numbers of equal bits (S + K) / 2.  x of at most 4 GiB.
 bool experts_tile_supported(const ExpertsArgs& a);
 hipError_t launch_experts_tile(const ExpertsArgs& a, uint16_t* counts, hipStream_t s);
+// The same for few rows per expert (experts_skinny.hip).
+hipError_t launch_experts_skinny(const ExpertsArgs& a, uint16_t* counts, hipStream_t s);
+// y from the counts (experts_combine.hip).
+hipError_t launch_experts_combine(const ExpertsArgs& a, const uint16_t* counts, hipStream_t s);
 
 size_t experts_sum_workspace(const bnn_experts_desc& d);
 hipError_t launch_experts_sum(const ExpertsArgs& a, hipStream_t s);

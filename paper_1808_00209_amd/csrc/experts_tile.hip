@@ -36,8 +36,7 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, c = lane & 31;
-  const GroupTile gt = group_tile(a.offsets, a.E, a.M, COUNTS ? a.E - 1 : a.E, a.rlog, a.cols,
-                                  blockIdx.x, gridDim.x);
+  const GroupTile gt = group_tile(a.offsets, a.E, a.M, !COUNTS, a.rlog, a.cols, blockIdx.x);
   if (gt.group < 0) return;
   const int rows = min(gt.end - gt.begin, 1 << a.rlog);
   auto pair_at = [&](int i) {  // the pair at row i of the tile (rows past it: the last one)
@@ -58,7 +57,6 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
   TileLoop t;
   t.ra = tile_rsrc(a.x, a.x_bytes);
   t.rb = tile_rsrc(a.w + static_cast<size_t>(gt.group) * a.N * a.Kw, a.w_bytes);
-  t.aoff = (static_cast<uint32_t>(pair_at(tid >> 1) / a.share) * a.Kw + 4 * (tid & 1)) * 4;
 #pragma unroll
   for (int tf = 0; tf < 2; ++tf)
     t.woff[tf] = (static_cast<uint32_t>(f0 + 32 * tf + c) * a.Kw + 4 * h) * 4;
@@ -86,7 +84,9 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
   for (int tf = 0; tf < 2; ++tf)
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt) acc[tf][pt] = v16f{};
-  tile_loop<PT>(acc, act, t);
+  tile_loop<PT>(acc, act, t, [&] {
+    return (static_cast<uint32_t>(pair_at(tid >> 1) / a.share) * a.Kw + 4 * (tid & 1)) * 4;
+  });
   int pair[PT];  // (read here: kept through the loop they cost registers that it spills)
 #pragma unroll
   for (int pt = 0; pt < PT; ++pt) pair[pt] = pair_at((t.wpi * PT + pt) * 32 + c);

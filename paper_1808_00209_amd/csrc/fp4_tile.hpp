@@ -38,7 +38,6 @@ __device__ __forceinline__ v4i tile_load4(__amdgpu_buffer_rsrc_t r, uint32_t vof
 // of a chunk in both operands, one 16-byte load per row and half.
 struct TileLoop {
   __amdgpu_buffer_rsrc_t ra, rb;  // data rows and weight rows
-  uint32_t aoff;     // byte offset of row tid / 2 of the block's 128, + 16 (tid % 2)
   uint32_t woff[2];  // byte offsets of weight rows f0 + c and f0 + 32 + c, + 16 h
   int32_t K, Kw;     // bits and words of a row
   int32_t chunks;    // of 8 words
@@ -48,9 +47,12 @@ struct TileLoop {
 
 // acc[tf][pt] += the 32 x 32 sums of outputs f0 + 32 tf and rows
 // 32 (wpi PT + pt) .. (register e of lane (h, c): output 8 (e / 4) + 4 h +
-// e % 4, row c).  Every thread of the workgroup takes part.
-template <int PT>
-__device__ __forceinline__ void tile_loop(v16f (&acc)[2][PT], v4i* act, const TileLoop& t) {
+// e % 4, row c).  Every thread of the workgroup takes part.  row_off() is the
+// byte offset of row tid / 2 of the block's 128 in ra, + 16 (tid % 2): called
+// after the first weight loads, which need not wait for what it reads.
+template <int PT, class RowOff>
+__device__ __forceinline__ void tile_loop(v16f (&acc)[2][PT], v4i* act, const TileLoop& t,
+                                          RowOff&& row_off) {
   constexpr int kRing = PT == 4 ? 2 : 4;  // chunks of words in flight
   constexpr int buf1 = kTileRows * kTilePS;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
@@ -84,8 +86,9 @@ __device__ __forceinline__ void tile_loop(v16f (&acc)[2][PT], v4i* act, const Ti
   };
 
   v4i xr[kRing], wr[kRing][2];  // words of the next kRing chunks, in flight
+  uint32_t aoff;
   auto load_x = [&](int r, int ch) {
-    xr[r] = tile_load4(t.ra, t.aoff, static_cast<uint32_t>(ch) * 32);
+    xr[r] = tile_load4(t.ra, aoff, static_cast<uint32_t>(ch) * 32);
   };
   auto load_w = [&](int r, int ch) {
 #pragma unroll
@@ -93,10 +96,11 @@ __device__ __forceinline__ void tile_loop(v16f (&acc)[2][PT], v4i* act, const Ti
       wr[r][tf] = tile_load4(t.rb, t.woff[tf], static_cast<uint32_t>(ch) * 32);
   };
 #pragma unroll
-  for (int r = 0; r < kRing; ++r) {
-    load_x(r, min(r, nch - 1));
-    load_w(r, min(r, nch - 1));
-  }
+  for (int r = 0; r < kRing; ++r) load_w(r, min(r, nch - 1));
+  __builtin_amdgcn_sched_barrier(0);
+  aoff = row_off();
+#pragma unroll
+  for (int r = 0; r < kRing; ++r) load_x(r, min(r, nch - 1));
   int abase[PT];
 #pragma unroll
   for (int pt = 0; pt < PT; ++pt) abase[pt] = ((t.wpi * PT + pt) * 32 + c) * kTilePS + 4 * h;

@@ -26,28 +26,39 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
-// The tile of block `block` of `grid` (a multiple of 8): every group's rows
-// are cut into tiles of R = 1 << rlog positions, each with `cols` column
-// tiles, column tiles fastest; groups 0 .. last are counted (last = G - 1, or G
-// to cover the rows of no group too).  Block b runs on XCD b mod 8, and an XCD
-// takes consecutive tiles, so that its L2 serves a row tile's rows and a
-// group's weights to several of them.  Wave-uniform; every lane of a wave has
-// to call it.  Offsets out of range are clamped.
+// The tile of block `block` (of a grid that is a multiple of 8): every group's
+// rows are cut into tiles of 1 << rlog positions, each with `cols` column
+// tiles, column tiles fastest; with `rest`, the rows of no group come as tiles
+// of group G after the others.  Block b runs on XCD b mod 8, and an XCD takes
+// consecutive tiles, so that its L2 serves a row tile's rows and a group's
+// weights to several of them.  Wave-uniform; every lane of a wave has to call
+// it.  Offsets out of range are clamped.
 __device__ __forceinline__ GroupTile group_tile(const int32_t* __restrict__ offsets, int G, int M,
-                                                int last, int rlog, uint32_t cols, uint32_t block,
-                                                uint32_t grid) {
+                                                bool rest, int rlog, uint32_t cols,
+                                                uint32_t block) {
   const int lane = threadIdx.x & 63;
-  auto at = [&](int g) { return g > G ? M : min(max(offsets[g], 0), M); };
-  auto tiles = [&](int g) {
-    return g > last ? 0 : (max(at(g + 1) - at(g), 0) + (1 << rlog) - 1) >> rlog;
+  const int round = (1 << rlog) - 1;
+  // 64 groups at a time, one per lane: first position, end and tiles.
+  int b = 0, e = 0, mine = 0, scan = 0;
+  auto batch = [&](int g0) {
+    const int g = g0 + lane;
+    b = offsets[min(g, G)];
+    e = offsets[min(g + 1, G)];
+    b = min(max(b, 0), M);
+    e = min(max(e, b), M);
+    mine = (e - b + round) >> rlog;  // (0 from group G on)
+    scan = wave_scan(mine);
   };
-  // One batch of 64 groups keeps its values; more are read again below.
-  int mine = tiles(lane);
-  int scan = wave_scan(mine);
-  int total = __builtin_amdgcn_readlane(scan, 63);
-  for (int g0 = 64; g0 <= last; g0 += 64)
-    total += __builtin_amdgcn_readlane(wave_scan(tiles(g0 + lane)), 63);
-  const uint32_t all = static_cast<uint32_t>(total) * cols;
+  int total = 0, g0 = 0;
+  for (;;) {
+    batch(g0);
+    total += __builtin_amdgcn_readlane(scan, 63);
+    if (g0 + 64 >= G) break;
+    g0 += 64;
+  }
+  const int done = __builtin_amdgcn_readlane(e, (G - 1) & 63);  // rows of all groups
+  const int tail = rest ? (M - done + round) >> rlog : 0;
+  const uint32_t all = static_cast<uint32_t>(total + tail) * cols;
   const uint32_t per = (all + 7) / 8;
   const uint32_t slot = block >> 3;
   const uint32_t t = (block & 7) * per + slot;
@@ -55,21 +66,30 @@ __device__ __forceinline__ GroupTile group_tile(const int32_t* __restrict__ offs
   if (slot >= per || t >= all) return r;
   int row = static_cast<int>(t / cols);
   r.col = t - static_cast<uint32_t>(row) * cols;
-  for (int g0 = 0;;) {
+  if (row >= total) {
+    r.group = G;
+    r.begin = done + ((row - total) << rlog);
+    r.end = M;
+    return r;
+  }
+  if (g0 > 0) {  // (several batches: the last one is held)
+    g0 = 0;
+    batch(0);
+  }
+  for (;;) {
     const uint64_t hit = __ballot(scan > row);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       r.group = g0 + l;
-      const int before = __builtin_amdgcn_readlane(scan - mine, l);
-      r.begin = __builtin_amdgcn_readfirstlane(at(r.group)) + ((row - before) << rlog);
-      r.end = __builtin_amdgcn_readfirstlane(at(r.group + 1));
+      r.begin = __builtin_amdgcn_readlane(b, l) +
+                ((row - __builtin_amdgcn_readlane(scan - mine, l)) << rlog);
+      r.end = __builtin_amdgcn_readlane(e, l);
       return r;
     }
     row -= __builtin_amdgcn_readlane(scan, 63);
     g0 += 64;
-    if (g0 > last) return r;
-    mine = tiles(g0 + lane);
-    scan = wave_scan(mine);
+    if (g0 >= G) return r;  // (not reached: row < total)
+    batch(g0);
   }
 }
 

@@ -267,7 +267,6 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
   TileLoop t;
   t.ra = tile_rsrc(g.bits, g.bits_bytes);
   t.rb = tile_rsrc(a.w, g.w_bytes);
-  t.aoff = (static_cast<uint32_t>(min(m00 + (tid >> 1), a.M - 1)) * g.Kw + 4 * (tid & 1)) * 4;
 #pragma unroll
   for (int tf = 0; tf < 2; ++tf)
     t.woff[tf] = (static_cast<uint32_t>(f0 + 32 * tf + c) * g.Kw + 4 * h) * 4;
@@ -281,7 +280,9 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
   for (int tf = 0; tf < 2; ++tf)
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt) acc[tf][pt] = v16f{};
-  tile_loop<PT>(acc, act, t);
+  tile_loop<PT>(acc, act, t, [&] {
+    return (static_cast<uint32_t>(min(m00 + (tid >> 1), a.M - 1)) * g.Kw + 4 * (tid & 1)) * 4;
+  });
 
   // y = alpha S + u b^T, one 32 x 32 tile after another; u b^T by 16 ranks at a
   // time and one adapter of the tile's rows after another, the rows of other
