@@ -35,23 +35,37 @@ constexpr int kDownRows = 16 * kDownRW;
 constexpr int kGroup = 128;            // k per step of a wave: 4 words of sign bits
 
 // A row's 32 consecutive elements as the four lane groups of a 16-row operand
-// hold them: lane (q, c) has elements 8 q .. 8 q + 7 of row c.  `left`: the
-// elements from 8 q on that exist (rows need no alignment beyond the type's).
+// hold them: lane (q, c) has elements 8 q .. 8 q + 7 of row c.
 template <class T>
 struct Frag {
   T v[8];
 };
 
-template <class T>
+// FULL: all 8 elements exist (rows need no alignment beyond the type's);
+// otherwise `left` of them do, and the others read 0.
+template <bool FULL, class T>
 __device__ __forceinline__ Frag<T> load_frag(const T* p, int left) {
   Frag<T> f;
-  if (left >= 8) {
+  if constexpr (FULL) {
     __builtin_memcpy(f.v, p, sizeof(f.v));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f.v[i] = i < left ? p[i] : T{};
   }
   return f;
+}
+
+// f where mask is ~0, zeros where it is 0.
+template <class T>
+__device__ __forceinline__ Frag<T> masked(const Frag<T>& f, uint32_t mask) {
+  constexpr int kWords = sizeof(Frag<T>) / 4;
+  uint32_t w[kWords];
+  __builtin_memcpy(w, f.v, sizeof(w));
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) w[i] &= mask;
+  Frag<T> r;
+  __builtin_memcpy(r.v, w, sizeof(w));
+  return r;
 }
 
 __device__ __forceinline__ v4f mma16(const Frag<__bf16>& x, const Frag<__bf16>& y, v4f acc) {
@@ -78,6 +92,8 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
                                                             uint32_t* __restrict__ bits,
                                                             int slices) {
   __shared__ float part[kDownNW][kDownRows][16 * NR + 4];
+  __shared__ int32_t adapter[kDownRows], adapters;
+  __shared__ uint32_t adapter_rows[kDownRows];
   const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int p0 = blockIdx.x * kDownRows, slice = blockIdx.y, r0 = blockIdx.z * 16 * NR;
@@ -94,82 +110,140 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
     xr[i] = static_cast<const T*>(a.x) + row * a.x_stride + 8 * q;
     id[i] = p < a.M ? adapter_of(a, row) : -1;
   }
-  v4f acc[kDownRW][NR] = {};
-  // One pass over the slice per adapter among the block's rows (mostly one);
-  // the first pass, with or without an adapter, makes the sign bits.
-  uint32_t todo = 0;  // bit 16 i + c: the row still waits for its adapter
+  // The adapters among the block's rows, each with its rows (bit 16 i + c).
+  if (wave == 0) {
+    uint32_t todo = 0;
 #pragma unroll
-  for (int i = 0; i < kDownRW; ++i)
-    todo |= static_cast<uint32_t>(__ballot(id[i] >= 0) & 0xFFFFu) << (16 * i);
-  for (bool first = true; first || todo; first = false) {
-    int l = -1;
-    if (todo) {
+    for (int i = 0; i < kDownRW; ++i)
+      todo |= static_cast<uint32_t>(__ballot(id[i] >= 0) & 0xFFFFu) << (16 * i);
+    int n = 0;
+    for (; todo; ++n) {
       const int at = __builtin_ctz(todo);
-      l = __builtin_amdgcn_readlane(at < 16 ? id[0] : id[1], at & 15);
-    } else if (!want_bits) {
-      break;
+      const int l = __builtin_amdgcn_readlane(at < 16 ? id[0] : id[1], at & 15);
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < kDownRW; ++i)
+        m |= static_cast<uint32_t>(__ballot(id[i] == l) & 0xFFFFu) << (16 * i);
+      todo &= ~m;
+      if (lane == 0) {
+        adapter[n] = l;
+        adapter_rows[n] = m;
+      }
     }
-    bool mine[kDownRW];
+    if (lane == 0) adapters = n;
+  }
+  typedef Frag<T> Xs[4][kDownRW];
+  typedef Frag<T> As[4][NR];
+  v4f acc[kDownRW][NR] = {};
+  auto load_x = [&](Xs& x, int g, auto full) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int i = 0; i < kDownRW; ++i) {
+        const int k = g * kGroup + 32 * s;
+        x[s][i] = load_frag<decltype(full)::value, T>(xr[i] + k, a.K - k - 8 * q);
+      }
+  };
+  auto load_a = [&](As& w, int d, int g, auto full) {
+    const T* ar = static_cast<const T*>(a.a) +
+                  static_cast<size_t>(__builtin_amdgcn_readfirstlane(adapter[d])) * a.rank * a.K +
+                  8 * q;
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int r = r0 + 16 * n + c;  // (past the last rank: read rank 0, dropped at the end)
+      const T* src = ar + static_cast<size_t>(r < a.rank ? r : 0) * a.K;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int k = g * kGroup + 32 * s;
+        w[s][n] = load_frag<decltype(full)::value, T>(src + k, a.K - k - 8 * q);
+      }
+    }
+  };
+  auto multiply = [&](const Xs& x, const As& w, int d) {
+    const uint32_t rows = adapter_rows[d];
 #pragma unroll
     for (int i = 0; i < kDownRW; ++i) {
-      mine[i] = l >= 0 && id[i] == l;
-      todo &= ~(static_cast<uint32_t>(__ballot(mine[i]) & 0xFFFFu) << (16 * i));
-    }
-    const T* ar = static_cast<const T*>(a.a) +
-                  (static_cast<size_t>(max(l, 0)) * a.rank + r0 + c) * a.K + 8 * q;
-    for (int g = slice * kDownNW + wave; g < groups; g += slices * kDownNW) {
-      Frag<T> x[4][kDownRW];
+      const uint32_t mine = (rows >> (16 * i + c)) & 1 ? ~0u : 0u;
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int s = 0; s < 4; ++s) {
+        const Frag<T> xm = masked(x[s][i], mine);
 #pragma unroll
-        for (int i = 0; i < kDownRW; ++i) {
-          const int k = g * kGroup + 32 * s;
-          x[s][i] = load_frag<T>(xr[i] + k, a.K - k - 8 * q);
-        }
-      if (l >= 0) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const int k = g * kGroup + 32 * s;
-          Frag<T> xm[kDownRW];
-#pragma unroll
-          for (int i = 0; i < kDownRW; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) xm[i].v[e] = mine[i] ? x[s][i].v[e] : T{};
-#pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            const Frag<T> w = load_frag<T>(ar + static_cast<size_t>(16 * n) * a.K + k,
-                                           r0 + 16 * n + c < a.rank ? a.K - k - 8 * q : 0);
-#pragma unroll
-            for (int i = 0; i < kDownRW; ++i) acc[i][n] = mma16(w, xm[i], acc[i][n]);
-          }
-        }
-      }
-      if (first && want_bits) {
-        float off[4][8];
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int k = g * kGroup + 32 * s + 8 * q + e;
-            off[s][e] = a.offset && k < a.K ? a.offset[k] : 0.0f;
-          }
-#pragma unroll
-        for (int i = 0; i < kDownRW; ++i) {
-          uint32_t w[4];
-#pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            uint32_t byte = 0;  // (elements past K are 0 with offset 0: bit 0)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              byte = 2 * byte + (to_f32(x[s][i].v[e]) + off[s][e] > 0.0f ? 1u : 0u);
-            w[s] = byte << (24 - 8 * q);
-          }
-          const uint32_t word = or_rows4(w[0], w[1], w[2], w[3]);  // lane (q, c): word q
-          const int p = p0 + 16 * i + c, wi = 4 * g + q;
-          if (p < a.M && wi < kw) bits[static_cast<size_t>(p) * kw + wi] = word;
-        }
+        for (int n = 0; n < NR; ++n) acc[i][n] = mma16(w[s][n], xm, acc[i][n]);
       }
     }
+  };
+  auto make_bits = [&](const Xs& x, int g, auto full) {
+    uint32_t w[kDownRW][4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int k = g * kGroup + 32 * s + 8 * q;
+      Frag<float> off = {};
+      if (a.offset) off = load_frag<decltype(full)::value, float>(a.offset + k, a.K - k);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) off.v[e] += 0.0f;  // -0 to +0
+#pragma unroll
+      for (int i = 0; i < kDownRW; ++i) {
+        // A finite sum is above 0 where its pattern is, as a whole number (it
+        // is not -0: off has none); then 0 - pattern has the sign bit.
+        // Elements past K are 0 with offset 0: bit 0.
+        uint32_t byte = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          byte = __builtin_amdgcn_alignbit(
+              byte, 0u - __float_as_uint(to_f32(x[s][i].v[e]) + off.v[e]), 31);
+        w[i][s] = byte << (24 - 8 * q);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kDownRW; ++i) {
+      // lane (q, c): word q of row c
+      const uint32_t word = or_rows4(w[i][0], w[i][1], w[i][2], w[i][3]);
+      const int p = p0 + 16 * i + c, wi = 4 * g + q;
+      if (p < a.M && wi < kw) bits[static_cast<size_t>(p) * kw + wi] = word;
+    }
+  };
+
+  // Whole groups, the next one's x in flight, and up to 16 ranks the next
+  // adapter's rows; then what is left of K.
+  // (consecutive groups of a wave: 34 us for the 8192 rows below, against 37
+  // with the waves' groups interleaved)
+  const int per = (groups + slices * kDownNW - 1) / (slices * kDownNW);
+  int g = (slice * kDownNW + wave) * per;
+  const int end = min(g + per, groups), whole = min(a.K / kGroup, end);
+  constexpr bool kAhead = NR == 1;
+  Xs x;
+  As w;
+  if (g < whole) load_x(x, g, std::true_type{});
+  __syncthreads();
+  const int nd = __builtin_amdgcn_readfirstlane(adapters);
+  if (g < whole) {
+    if (kAhead && nd) load_a(w, 0, g, std::true_type{});
+    for (; g < whole; ++g) {
+      Xs next;
+      load_x(next, min(g + 1, whole - 1), std::true_type{});
+      for (int d = 0; d < nd; ++d) {
+        if constexpr (kAhead) {
+          As after;
+          const bool last = d + 1 == nd;
+          load_a(after, last ? 0 : d + 1, last ? min(g + 1, whole - 1) : g, std::true_type{});
+          multiply(x, w, d);
+          __builtin_memcpy(&w, &after, sizeof(w));
+        } else {
+          load_a(w, d, g, std::true_type{});
+          multiply(x, w, d);
+        }
+      }
+      if (want_bits) make_bits(x, g, std::true_type{});
+      __builtin_memcpy(&x, &next, sizeof(x));
+    }
+  }
+  if (g < end) {
+    load_x(x, g, std::false_type{});
+    for (int d = 0; d < nd; ++d) {
+      load_a(w, d, g, std::false_type{});
+      multiply(x, w, d);
+    }
+    if (want_bits) make_bits(x, g, std::false_type{});
   }
   // The waves' parts of u meet in LDS, added in the waves' order.
 #pragma unroll
@@ -225,25 +299,36 @@ __device__ __forceinline__ void split_frag(const float (&v)[8], bool keep, v8bf 
   for (int i = 0; i < P; ++i) out[i] = bf16x8(b[i]);
 }
 
-// Lane (h, c)'s share of 16 ranks of output row n: b[l][n][16 rc + 8 h ..],
-// 0 past the rank or N.
+// Lane (h, c)'s share of 16 ranks: b[l][n][r .. r + 7] of an output n (past the
+// rank or N: other values, dropped by split_b), as it lies in memory.
 template <class T>
-__device__ __forceinline__ void load_b(const LoraArgs& a, int l, int n, int r,
-                                       v8bf (&out)[kParts<T>]) {
+struct RawB {
+  T v[8];
+};
+
+template <class T>
+__device__ __forceinline__ RawB<T> load_b(const LoraArgs& a, int l, int n, int r) {
   const bool in = n < a.N && r < a.rank;
   const T* src = static_cast<const T*>(a.b) +
                  (in ? (static_cast<size_t>(l) * a.N + n) * a.rank + r : size_t{0});
-  T v[8];
-  __builtin_memcpy(v, __builtin_assume_aligned(src, sizeof(v) > 16 ? 16 : sizeof(v)), sizeof(v));
+  RawB<T> x;
+  __builtin_memcpy(x.v, __builtin_assume_aligned(src, 16), sizeof(x.v));
+  return x;
+}
+
+template <class T>
+__device__ __forceinline__ void split_b(const RawB<T>& x, bool keep, v8bf (&out)[kParts<T>]) {
   if constexpr (kParts<T> == 1) {
+    uint32_t w[4];
+    __builtin_memcpy(w, x.v, sizeof(w));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = in ? v[e] : T{};
-    __builtin_memcpy(&out[0], v, sizeof(v));
+    for (int i = 0; i < 4; ++i) w[i] = keep ? w[i] : 0u;
+    __builtin_memcpy(&out[0], w, sizeof(w));
   } else {
     float f[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = to_f32(v[e]);
-    split_frag<kParts<T>>(f, in, out);
+    for (int e = 0; e < 8; ++e) f[e] = to_f32(x.v[e]);
+    split_frag<kParts<T>>(f, keep, out);
   }
 }
 
@@ -284,73 +369,108 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
     return (static_cast<uint32_t>(min(m00 + (tid >> 1), a.M - 1)) * g.Kw + 4 * (tid & 1)) * 4;
   });
 
-  // y = alpha S + u b^T, one 32 x 32 tile after another; u b^T by 16 ranks at a
-  // time and one adapter of the tile's rows after another, the rows of other
-  // adapters entering as zeros, in sums of its own (S is exact: so alpha S is
-  // rounded once, whatever the adapters add up).  A row's outputs leave through
-  // LDS (a region per wave: 32 rows x 64 outputs) as one run.
-  constexpr int kStride = 68;  // LDS words per row
-  float* ts = reinterpret_cast<float*>(act) + wave * (32 * kStride);
+  // y = alpha S + u b^T, 32 rows after another.  u b^T takes 16 ranks at a time
+  // and one adapter of the rows after another, the rows of other adapters
+  // entering as zeros, in sums of its own (S is exact: so alpha S is rounded
+  // once, whatever the adapters add up).  While one such step multiplies, the
+  // next one's values are loaded, the next rows' first step among them.  A
+  // row's outputs leave through LDS (a region per wave) as one run.
+  constexpr int kStride = 68;  // LDS words per row of 64 outputs
+  float* ts = reinterpret_cast<float*>(act) + wave * (33 * kStride);
+  float* al = ts + 32 * kStride;  // alpha of the wave's 64 outputs
   constexpr int kV = 16 / sizeof(Y);  // outputs per 16-byte store
   constexpr int kLanes = 64 / kV;     // lanes per row
   const bool wide = a.N % kV == 0;
-  const __amdgpu_buffer_rsrc_t ral = tile_rsrc(a.alpha, a.alpha ? a.N * 4 : 0);
+  al[lane] = f0 + lane < a.N && a.alpha ? a.alpha[f0 + lane] : 1.0f;
+  const int base = m00 + t.wpi * PT * 32 + c;
+  int row[PT], id[PT];
+#pragma unroll
+  for (int pt = 0; pt < PT; ++pt) row[pt] = row_of(a, base + 32 * pt);
+#pragma unroll
+  for (int pt = 0; pt < PT; ++pt) id[pt] = base + 32 * pt < a.M ? adapter_of(a, row[pt]) : -1;
+
+  RawB<T> nb[2];
+  float nu[8];
+  auto fetch = [&](int l, int r, int mine, int p) {
+    const int rr = r + 8 * h;
+#pragma unroll
+    for (int tf = 0; tf < 2; ++tf) nb[tf] = load_b<T>(a, l, f0 + 32 * tf + c, rr);
+    const bool in = mine == l && rr < a.rank;
+    const float* src = g.u + (in ? static_cast<size_t>(p) * a.rank + rr : size_t{0});
+    __builtin_memcpy(nu, __builtin_assume_aligned(src, 16), sizeof(nu));
+    for (int s = 1; s < g.slices; ++s) {
+      float w[8];
+      __builtin_memcpy(
+          w, __builtin_assume_aligned(src + static_cast<size_t>(s) * a.M * a.rank, 16), sizeof(w));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) nu[e] += w[e];
+    }
+  };
+  auto waiting = [&](int pt) { return static_cast<uint32_t>(__ballot(id[pt] >= 0)); };
+  auto first_of = [&](int pt, uint32_t rows) {
+    return __builtin_amdgcn_readlane(id[pt], __builtin_ctz(rows));
+  };
+  if (const uint32_t rows = waiting(0)) fetch(first_of(0, rows), 0, id[0], base);
 #pragma unroll
   for (int pt = 0; pt < PT; ++pt) {
-    asm volatile("" ::: "memory");  // (no loads of later tiles up here: registers)
-    const int p0 = m00 + (t.wpi * PT + pt) * 32, p = p0 + c;
-    const int id = p < a.M ? adapter_of(a, row_of(a, p)) : -1;
+    asm volatile("" ::: "memory");  // (no loads of later rows up here: registers)
+    uint32_t todo = waiting(pt);
+    const uint32_t next_rows = pt + 1 < PT ? waiting(pt + 1 < PT ? pt + 1 : pt) : 0u;
+    auto fetch_next_rows = [&] {
+      if (pt + 1 < PT && next_rows) {
+        const int q = pt + 1 < PT ? pt + 1 : pt;
+        fetch(first_of(q, next_rows), 0, id[q], base + 32 * q);
+      }
+    };
+    v16f low[2] = {};
+    if (!todo) fetch_next_rows();
+    while (todo) {
+      const int l = first_of(pt, todo);
+      todo &= ~static_cast<uint32_t>(__ballot(id[pt] == l));
+      for (int r = 0; r < a.rank; r += 16) {
+        v8bf b[2][kParts<T>], u[3];
 #pragma unroll
-    for (int tf = 0; tf < 2; ++tf) {
-      uint32_t todo = static_cast<uint32_t>(__ballot(id >= 0));
-      v16f low = {};
-      while (todo) {
-        const int l = __builtin_amdgcn_readlane(id, __builtin_ctz(todo));
-        todo &= ~static_cast<uint32_t>(__ballot(id == l));
-        for (int r = 0; r < a.rank; r += 16) {
-          const int rr = r + 8 * h;
-          v8bf b[kParts<T>];
-          load_b<T>(a, l, f0 + 32 * tf + c, rr, b);
-          const bool mine = id == l && rr < a.rank;
-          float v[8] = {};
-          for (int s = 0; s < g.slices; ++s) {
-            const float* src =
-                g.u + (mine ? (static_cast<size_t>(s) * a.M + p) * a.rank + rr : size_t{0});
-            float w[8];
-            __builtin_memcpy(w, __builtin_assume_aligned(src, 16), sizeof(w));
+        for (int tf = 0; tf < 2; ++tf)
+          split_b<T>(nb[tf], f0 + 32 * tf + c < a.N && r + 8 * h < a.rank, b[tf]);
+        split_frag<3>(nu, id[pt] == l && r + 8 * h < a.rank, u);
+        if (r + 16 < a.rank)
+          fetch(l, r + 16, id[pt], base + 32 * pt);
+        else if (todo)
+          fetch(first_of(pt, todo), 0, id[pt], base + 32 * pt);
+        else
+          fetch_next_rows();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += w[e];
-          }
-          v8bf uf[3];
-          split_frag<3>(v, mine, uf);
+        for (int tf = 0; tf < 2; ++tf)
 #pragma unroll
           for (int i = kParts<T> - 1; i >= 0; --i)
 #pragma unroll
             for (int j = 2; j >= 0; --j)
               if (i + j < 4)
-                low = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[i], uf[j], low, 0, 0, 0);
-        }
-      }
-      // Register e of a tile holds output 8 (e / 4) + 4 h + e % 4 (past N: 0).
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const v4i v = tile_load4(ral, (f0 + 32 * tf + 2 * e + 4 * h) * 4, 0);
-        float y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          y[i] = acc[tf][pt][e + i] * (a.alpha ? __int_as_float(v[i]) : 1.0f) + low[e + i];
-        *reinterpret_cast<float4*>(&ts[c * kStride + 32 * tf + 2 * e + 4 * h]) =
-            float4{y[0], y[1], y[2], y[3]};
+                low[tf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[tf][i], u[j], low[tf], 0, 0,
+                                                                 0);
       }
     }
+    // Register e of a tile holds output 8 (e / 4) + 4 h + e % 4 of row c.
+#pragma unroll
+    for (int tf = 0; tf < 2; ++tf)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int n = 32 * tf + 2 * e + 4 * h;
+        const float4 f = *reinterpret_cast<const float4*>(&al[n]);
+        *reinterpret_cast<float4*>(&ts[c * kStride + n]) =
+            float4{acc[tf][pt][e] * f.x + low[tf][e], acc[tf][pt][e + 1] * f.y + low[tf][e + 1],
+                   acc[tf][pt][e + 2] * f.z + low[tf][e + 2],
+                   acc[tf][pt][e + 3] * f.w + low[tf][e + 3]};
+      }
 #pragma unroll
     for (int o = 0; o < 32; o += 64 / kLanes) {
       const int i = o + lane / kLanes, col = kV * (lane % kLanes), n = f0 + col;
+      const int m = __shfl(row[pt], i);
       Y v[kV];
 #pragma unroll
       for (int e = 0; e < kV; ++e) v[e] = from_f32<Y>(ts[i * kStride + col + e]);
-      if (p0 + i < a.M) {
-        Y* dst = static_cast<Y*>(a.y) + static_cast<size_t>(row_of(a, p0 + i)) * a.N + n;
+      if (base - c + 32 * pt + i < a.M) {
+        Y* dst = static_cast<Y*>(a.y) + static_cast<size_t>(m) * a.N + n;
         if (wide) {
           if (n < a.N) __builtin_memcpy(__builtin_assume_aligned(dst, 16), v, 16);
         } else {
@@ -363,12 +483,12 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
   }
 }
 
-// k slices of the down pass: enough blocks to fill the chip at few rows, at
-// least one group of 128 k for every wave.
+// k slices of the down pass: a block per compute unit (two: 37 against 34 us
+// for 8192 rows of 4096), at least one group of 128 k for every wave.
 int down_slices(int64_t M, int32_t K, int32_t rank) {
   const int64_t blocks = (M + kDownRows - 1) / kDownRows * ((rank + 63) / 64);
   const int64_t most = (K + kGroup * kDownNW - 1) / (kGroup * kDownNW);
-  const int64_t want = (512 + blocks - 1) / blocks;
+  const int64_t want = (256 + blocks - 1) / blocks;
   return static_cast<int>(want < most ? want : most);
 }
 
@@ -408,7 +528,7 @@ hipError_t launch_lora_tile(const LoraArgs& a, hipStream_t s) {
   g.row_tiles = (a.M + rows - 1) / rows;
   const unsigned grid =
       static_cast<unsigned>((static_cast<int64_t>(g.cols) * g.row_tiles + 7) / 8 * 8);
-  static_assert(kTileLds >= size_t{4} * 32 * 68 * 4, "the output tiles fit");
+  static_assert(kTileLds >= size_t{4} * 33 * 68 * 4, "the output tiles fit");
   with_real_type(a.dtype, [&](auto v) {
     using T = decltype(v);
     const unsigned bx = static_cast<unsigned>((a.M + kDownRows - 1) / kDownRows);

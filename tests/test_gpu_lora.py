@@ -114,10 +114,13 @@ def test_zeros_and_ties_of_the_offset_read_minus_one():
     w = np.full((N, 2), -1, np.int32)  # all +1
     p = dict(x=x, ids=np.full(3, -1, np.int32), w=w, a=torch.zeros(1, 8, K), b=torch.zeros(1, N, 8),
              scale=np.ones(1, np.float32), alpha=np.ones(N, np.float32), offset=offset)
-    y = _call(p)
-    assert y[0].tolist() == [-64.0] * N
-    assert y[1].tolist() == [0.0] * N
-    assert y[2].tolist() == [0.0] * N
+    for rows in (3, 40):  # few rows and more
+        q = dict(p, x=x.repeat(14, 1)[:rows], ids=np.full(rows, -1, np.int32))
+        y = _call(q)
+        for m in range(rows):
+            assert y[m].tolist() == [[-64.0] * N, [0.0] * N, [0.0] * N][m % 3]
+        q = dict(q, x=torch.full((rows, K), -0.0), offset=np.full(K, -0.0, np.float32))
+        assert _call(q).tolist() == [[-64.0] * N] * rows
 
 
 def test_strided_rows():
