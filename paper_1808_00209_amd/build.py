@@ -24,7 +24,7 @@ SOURCES = ["pack.hip", "bconv_valu.hip", "bconv_mfma.hip", "bconv_tile.hip", "bc
            "bfc_pair.hip", "bfc_gemm.hip", "bfc_tile.hip", "route.hip", "group_rows.hip",
            "experts.hip", "experts_tile.hip", "experts_skinny.hip",
            "experts_combine.hip",
-           "lora.hip", "lora_tile.hip", "api.cpp", "experts_api.cpp"]
+           "lora.hip", "lora_tile.hip", "lora_skinny.hip", "api.cpp", "experts_api.cpp"]
 ARCH = os.environ.get("BNN_OFFLOAD_ARCH", "gfx950")
 
 COMMON = [

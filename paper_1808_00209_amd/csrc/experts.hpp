@@ -74,5 +74,10 @@ hipError_t launch_bgemm_lora(const LoraArgs& a, hipStream_t s);
 size_t lora_tile_workspace(int64_t M, int32_t K, int32_t rank);
 bool lora_tile_supported(const LoraArgs& a);
 hipError_t launch_lora_tile(const LoraArgs& a, hipStream_t s);
+// Its two steps for few rows (lora_skinny.hip): u [M][rank] and sign bits, and
+// y from them (u as `slices` partial sums).
+void launch_lora_down_rows(const LoraArgs& a, float* u, uint32_t* bits, hipStream_t s);
+void launch_lora_up_skinny(const LoraArgs& a, const float* u, const uint32_t* bits, int slices,
+                           hipStream_t s);
 
 }  // namespace bnn

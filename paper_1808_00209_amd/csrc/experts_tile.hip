@@ -1,6 +1,7 @@
 // Binary FC layers of experts on the fp4 matrix cores (bnn_experts_fc, and the
 // products of bnn_experts_sum): one GEMM tile of fp4_tile.hpp per row tile of
 // an expert and 64, 128 or 256 outputs, the rows gathered through the order.
+#include "expert_plans.hpp"
 #include "experts.hpp"
 #include "fp4_tile.hpp"
 #include "group_tiles.hpp"
@@ -176,15 +177,15 @@ hipError_t launch_experts_tile(const ExpertsArgs& a, uint16_t* counts, hipStream
   e.share = a.share;
   e.x_bytes = static_cast<uint32_t>(static_cast<int64_t>(a.M / a.share) * e.Kw * 4);
   e.w_bytes = static_cast<uint32_t>(static_cast<int64_t>(a.N) * e.Kw * 4);
-  // Waves along the outputs, as many as there are 64-output tiles; then row
-  // tiles of 32, 64 or 128 by the rows that an expert has on average.
-  const int64_t avg = (a.M + a.E - 1) / a.E;
-  e.wfl = a.N > 128 ? 2 : a.N > 64 ? 1 : 0;
-  int pt = avg > 64 ? 4 : avg > 32 ? 2 : 1;
-  pt = pt < (1 << e.wfl) ? pt : 1 << e.wfl;
-  const int rows = (4 >> e.wfl) * pt * 32;
+  // Row tiles: the whole ones and, for every expert that has rows, half a tile.
+  const double some = a.E < a.M ? a.E : a.M;
+  const TileShape shape = tile_shape(a.N, e.chunks, 10000, 500, [&](int rows) {
+    return static_cast<double>(a.M) / rows + some / 2 + (some < 2 ? 0.5 : 0.0);
+  });
+  e.wfl = shape.wfl;
+  const int rows = shape.rows();
   e.rlog = rows == 128 ? 7 : rows == 64 ? 6 : 5;
-  e.cols = static_cast<uint32_t>((a.N + (64 << e.wfl) - 1) / (64 << e.wfl));
+  e.cols = static_cast<uint32_t>((a.N + shape.outputs() - 1) / shape.outputs());
   const int64_t tiles = group_tiles_bound(a.M, a.E + 1, rows) * e.cols;
   const unsigned grid = static_cast<unsigned>((tiles + 7) / 8 * 8);
   static_assert(kTileLds >= size_t{4} * 32 * kCountStride * 2, "the counts tiles fit");
@@ -195,7 +196,7 @@ hipError_t launch_experts_tile(const ExpertsArgs& a, uint16_t* counts, hipStream
     else
       experts_tile_kernel<PT, false><<<grid, kTileNT, kTileLds, s>>>(e);
   };
-  switch (pt) {
+  switch (shape.pt) {
     case 4: launch(std::integral_constant<int, 4>{}); break;
     case 2: launch(std::integral_constant<int, 2>{}); break;
     default: launch(std::integral_constant<int, 1>{}); break;

@@ -80,9 +80,7 @@ size_t lora_workspace(const bnn_lora_desc& d) {
 }
 
 hipError_t launch_bgemm_lora(const LoraArgs& a, hipStream_t s) {
-  // Up to 32 rows the matrix-core kernels have too few blocks: 32 rows, 4096 ->
-  // 4096, 28 adapters of rank 16: 143 us there, 87 us here.
-  if (options().algo != BNN_ALGO_VALU && a.M > 32 && lora_tile_supported(a)) return launch_lora_tile(a, s);
+  if (options().algo != BNN_ALGO_VALU && lora_tile_supported(a)) return launch_lora_tile(a, s);
   const LoraWs ws = split_ws(a);
   with_real_type(a.dtype, [&](auto v) {
     using T = decltype(v);

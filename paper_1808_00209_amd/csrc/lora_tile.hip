@@ -5,27 +5,16 @@
 // and u lie by position.  A row's sums are taken in an order that does not
 // hang on the rows beside it.
 #include "dtypes.hpp"
+#include "expert_plans.hpp"
 #include "experts.hpp"
 #include "fp4_tile.hpp"
 #include "lane_ops.hpp"
+#include "lora_parts.hpp"
 
 namespace bnn {
 namespace {
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ int row_of(const LoraArgs& a, int p) {
-  p = min(p, a.M - 1);
-  return a.order ? static_cast<int>(min(static_cast<uint32_t>(a.order[p]),
-                                        static_cast<uint32_t>(a.M - 1)))
-                 : p;
-}
-
-// The adapter of a row, -1 for none.
-__device__ __forceinline__ int adapter_of(const LoraArgs& a, int row) {
-  const int l = a.ids[row];
-  return l >= 0 && l < a.adapters ? l : -1;
-}
 
 // ------------------------------------------------------------ x -> bits, u ---
 constexpr int kDownNW = 8;             // waves, each an eighth of the block's k groups
@@ -106,9 +95,9 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
 #pragma unroll
   for (int i = 0; i < kDownRW; ++i) {
     const int p = p0 + 16 * i + c;
-    const int row = row_of(a, p);
+    const int row = lora_row(a, p);
     xr[i] = static_cast<const T*>(a.x) + row * a.x_stride + 8 * q;
-    id[i] = p < a.M ? adapter_of(a, row) : -1;
+    id[i] = p < a.M ? lora_adapter(a, row) : -1;
   }
   // The adapters among the block's rows, each with its rows (bit 16 i + c).
   if (wave == 0) {
@@ -256,7 +245,7 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
   for (int v = tid; v < kDownRows * 16 * NR; v += kDownNT) {
     const int i = v / (16 * NR), r = v % (16 * NR), p = p0 + i;
     if (p >= a.M || r0 + r >= a.rank) continue;
-    const int l = adapter_of(a, row_of(a, p));
+    const int l = lora_adapter(a, lora_row(a, p));
     if (l < 0) continue;
     float sum = part[0][i][r];
 #pragma unroll
@@ -267,13 +256,6 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
 }
 
 // --------------------------------------------------------- bits, u -> y ---
-// Parts of a value on the bf16 matrix cores: 1 (bf16), 2 (fp16: 11 significant
-// bits) or 3 (fp32), each product of u's three parts and these exact.
-template <class T>
-constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-template <>
-constexpr int kParts<_Float16> = 2;
-
 struct UpArgs {
   LoraArgs a;
   const float* u;
@@ -283,54 +265,6 @@ struct UpArgs {
   uint32_t cols;
   int32_t row_tiles;
 };
-
-// Eight values of u (or b) as bf16 operands, one per part.
-template <int P>
-__device__ __forceinline__ void split_frag(const float (&v)[8], bool keep, v8bf (&out)[P]) {
-  uint16_t b[3][8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const Split3 s = split3(keep ? v[e] : 0.0f);
-    b[0][e] = bf16_bits(s.p0);
-    b[1][e] = bf16_bits(s.p1);
-    b[2][e] = bf16_bits(s.p2);
-  }
-#pragma unroll
-  for (int i = 0; i < P; ++i) out[i] = bf16x8(b[i]);
-}
-
-// Lane (h, c)'s share of 16 ranks: b[l][n][r .. r + 7] of an output n (past the
-// rank or N: other values, dropped by split_b), as it lies in memory.
-template <class T>
-struct RawB {
-  T v[8];
-};
-
-template <class T>
-__device__ __forceinline__ RawB<T> load_b(const LoraArgs& a, int l, int n, int r) {
-  const bool in = n < a.N && r < a.rank;
-  const T* src = static_cast<const T*>(a.b) +
-                 (in ? (static_cast<size_t>(l) * a.N + n) * a.rank + r : size_t{0});
-  RawB<T> x;
-  __builtin_memcpy(x.v, __builtin_assume_aligned(src, 16), sizeof(x.v));
-  return x;
-}
-
-template <class T>
-__device__ __forceinline__ void split_b(const RawB<T>& x, bool keep, v8bf (&out)[kParts<T>]) {
-  if constexpr (kParts<T> == 1) {
-    uint32_t w[4];
-    __builtin_memcpy(w, x.v, sizeof(w));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = keep ? w[i] : 0u;
-    __builtin_memcpy(&out[0], w, sizeof(w));
-  } else {
-    float f[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = to_f32(x.v[e]);
-    split_frag<kParts<T>>(f, keep, out);
-  }
-}
 
 template <class T, class Y, int PT>
 __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
@@ -385,9 +319,9 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
   const int base = m00 + t.wpi * PT * 32 + c;
   int row[PT], id[PT];
 #pragma unroll
-  for (int pt = 0; pt < PT; ++pt) row[pt] = row_of(a, base + 32 * pt);
+  for (int pt = 0; pt < PT; ++pt) row[pt] = lora_row(a, base + 32 * pt);
 #pragma unroll
-  for (int pt = 0; pt < PT; ++pt) id[pt] = base + 32 * pt < a.M ? adapter_of(a, row[pt]) : -1;
+  for (int pt = 0; pt < PT; ++pt) id[pt] = base + 32 * pt < a.M ? lora_adapter(a, row[pt]) : -1;
 
   RawB<T> nb[2];
   float nu[8];
@@ -440,14 +374,7 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
         else
           fetch_next_rows();
 #pragma unroll
-        for (int tf = 0; tf < 2; ++tf)
-#pragma unroll
-          for (int i = kParts<T> - 1; i >= 0; --i)
-#pragma unroll
-            for (int j = 2; j >= 0; --j)
-              if (i + j < 4)
-                low[tf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[tf][i], u[j], low[tf], 0, 0,
-                                                                 0);
+        for (int tf = 0; tf < 2; ++tf) add_parts<T>(low[tf], b[tf], u);
       }
     }
     // Register e of a tile holds output 8 (e / 4) + 4 h + e % 4 of row c.
@@ -519,13 +446,23 @@ hipError_t launch_lora_tile(const LoraArgs& a, hipStream_t s) {
   g.w_bytes = static_cast<uint32_t>(static_cast<int64_t>(a.N) * g.Kw * 4);
   g.tmask = tail_mask(a.K);
   g.chunks = (g.Kw + 7) / 8;
-  g.slices = down_slices(a.M, a.K, a.rank);
-  g.wfl = a.N > 128 ? 2 : a.N > 64 ? 1 : 0;
-  int pt = a.M > 64 ? 4 : a.M > 32 ? 2 : 1;
-  pt = pt < (1 << g.wfl) ? pt : 1 << g.wfl;
-  const int rows = (4 >> g.wfl) * pt * 32;
-  g.cols = static_cast<uint32_t>((a.N + (64 << g.wfl) - 1) / (64 << g.wfl));
-  g.row_tiles = (a.M + rows - 1) / rows;
+  // A wave per row and rank component while all of them are few rounds of the
+  // chip (both steps, rows and then k tiles, in us: 32 rows x 4096, rank 16, 28
+  // adapters 14.2 and 38.1; 777 x 1100, rank 8 17.1 and 24.8; 512 x 4096, rank
+  // 16 23.5 and 26.3; 1024 x 4096, rank 16 27.4 and 24.6; 4096 x 1024, rank 8
+  // 28.2 and 20.7).
+  const bool few_rows = static_cast<int64_t>(a.M) * (a.rank + 1) <= 16384;
+  g.slices = few_rows ? 1 : down_slices(a.M, a.K, a.rank);
+  // K split over a workgroup per 32 x 32 tile while they are about three per
+  // compute unit (128 rows, 4096 -> 4096, many adapters 18.7 us, in the larger
+  // tiles 33.6; one per 16 rows, rank 64 21.8 and 25.5; 256 rows 27.1 and 26.6).
+  const bool few_tiles = (a.M + 31) / 32 * words_of(a.N) <= 800;
+  const TileShape shape = tile_shape(a.N, g.chunks, 7000, 2500, [&](int rows) {
+    return static_cast<double>((a.M + rows - 1) / rows);
+  });
+  g.wfl = shape.wfl;
+  g.cols = static_cast<uint32_t>((a.N + shape.outputs() - 1) / shape.outputs());
+  g.row_tiles = (a.M + shape.rows() - 1) / shape.rows();
   const unsigned grid =
       static_cast<unsigned>((static_cast<int64_t>(g.cols) * g.row_tiles + 7) / 8 * 8);
   static_assert(kTileLds >= size_t{4} * 33 * 68 * 4, "the output tiles fit");
@@ -533,16 +470,22 @@ hipError_t launch_lora_tile(const LoraArgs& a, hipStream_t s) {
     using T = decltype(v);
     const unsigned bx = static_cast<unsigned>((a.M + kDownRows - 1) / kDownRows);
     const unsigned by = static_cast<unsigned>(g.slices);
-    if (a.rank <= 16)
+    if (few_rows)
+      launch_lora_down_rows(a, u, bits, s);
+    else if (a.rank <= 16)
       lora_down_kernel<T, 1><<<dim3(bx, by, 1), kDownNT, 0, s>>>(a, u, bits, g.slices);
     else if (a.rank <= 32)
       lora_down_kernel<T, 2><<<dim3(bx, by, 1), kDownNT, 0, s>>>(a, u, bits, g.slices);
     else
       lora_down_kernel<T, 4><<<dim3(bx, by, static_cast<unsigned>((a.rank + 63) / 64)), kDownNT, 0,
                                s>>>(a, u, bits, g.slices);
+    if (few_tiles) {
+      launch_lora_up_skinny(a, u, bits, g.slices, s);
+      return;
+    }
     with_real_type(a.out_dtype, [&](auto y) {
       using Y = decltype(y);
-      switch (pt) {
+      switch (shape.pt) {
         case 4: lora_up_kernel<T, Y, 4><<<grid, kTileNT, kTileLds, s>>>(g); break;
         case 2: lora_up_kernel<T, Y, 2><<<grid, kTileNT, kTileLds, s>>>(g); break;
         default: lora_up_kernel<T, Y, 1><<<grid, kTileNT, kTileLds, s>>>(g); break;
