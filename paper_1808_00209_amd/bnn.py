@@ -562,9 +562,16 @@ def _real(dtype, name):
 
 
 def _shaped(t, shape, name):
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t is not None and t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, shape, tuple(t.shape)))
     return t
+
+
+def _output(t, like, shape, dtype, name):
+    """A new tensor on like's device, or the caller's, looked at."""
+    if t is None:
+        return like.new_empty(shape, dtype=dtype)
+    return _shaped(_dev(t, dtype, name), shape, name)
 
 
 def _rows(t, name):
@@ -574,10 +581,11 @@ def _rows(t, name):
     return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
 
 
-def _workspace(ws, need, device):
-    """The caller's workspace, or a new one of `need` bytes, and its size."""
+def _workspace(ws, need, like):
+    """The caller's workspace, or a new one of `need` bytes beside like, and its
+    size."""
     if ws is None:
-        return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
+        return (like.new_empty(need, dtype=torch.uint8) if need else None), need
     return ws, _dev(ws, torch.uint8, "workspace").numel()
 
 
@@ -596,12 +604,8 @@ def bnn_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=No
     stride = _rows(logits, "logits")
     T, E = logits.shape
     bias = _shaped(_dev(bias, torch.float32, "bias"), (E,), "bias")
-    if ids is None:
-        ids = torch.empty((T, top_k), dtype=torch.int32, device=logits.device)
-    if weights is None:
-        weights = torch.empty((T, top_k), dtype=torch.float32, device=logits.device)
-    _shaped(_dev(ids, torch.int32, "ids"), (T, top_k), "ids")
-    _shaped(_dev(weights, torch.float32, "weights"), (T, top_k), "weights")
+    ids = _output(ids, logits, (T, top_k), torch.int32, "ids")
+    weights = _output(weights, logits, (T, top_k), torch.float32, "weights")
     if score not in _SCORES:
         raise ValueError("score must be one of %s" % sorted(_SCORES))
     d = RouteDesc(E, top_k, groups, groups if top_groups is None else top_groups, group_top,
@@ -624,13 +628,9 @@ def bnn_group_rows(ids, G, offsets=None, order=None, workspace=None, stream=None
     lib = load()
     _dev(ids, torch.int32, "ids")
     M = ids.numel()
-    if offsets is None:
-        offsets = torch.empty(G + 1, dtype=torch.int32, device=ids.device)
-    if order is None:
-        order = torch.empty(M, dtype=torch.int32, device=ids.device)
-    _shaped(_dev(offsets, torch.int32, "offsets"), (G + 1,), "offsets")
-    _shaped(_dev(order, torch.int32, "order"), (M,), "order")
-    workspace, n = _workspace(workspace, bnn_group_rows_workspace_size(M, G), ids.device)
+    offsets = _output(offsets, ids, (G + 1,), torch.int32, "offsets")
+    order = _output(order, ids, (M,), torch.int32, "order")
+    workspace, n = _workspace(workspace, bnn_group_rows_workspace_size(M, G), ids)
     _check(lib.bnn_group_rows(M, G, _ptr(ids), _ptr(offsets), _ptr(order), _ptr(workspace), n,
                               _stream(stream)))
     return offsets, order
@@ -662,9 +662,7 @@ def bnn_experts_fc(x, K, w, offsets, order, thr, flip=None, out_bits=None, strea
     nw = words(d.N)
     _shaped(_dev(thr, torch.int32, "thr"), (d.E, d.N), "thr")
     _shaped(_dev(flip, torch.int32, "flip"), (d.E, nw), "flip")
-    if out_bits is None:
-        out_bits = torch.empty((M, nw), dtype=torch.int32, device=x.device)
-    _shaped(_u32(out_bits), (M, nw), "out_bits")
+    out_bits = _output(out_bits, x, (M, nw), torch.int32, "out_bits")
     _check(lib.bnn_experts_fc(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(offsets), _ptr(order),
                               _ptr(thr), _ptr(flip), _ptr(out_bits), _stream(stream)))
     return out_bits
@@ -688,11 +686,10 @@ def bnn_experts_sum(x, K, w, ids, weights, offsets, order, alpha=None, dtype=tor
     _shaped(_dev(weights, torch.float32, "weights"), (T, top_k), "weights")
     d = _experts_desc(x, K, w, T * top_k, top_k, offsets, order)
     _shaped(_dev(alpha, torch.float32, "alpha"), (d.E, d.N), "alpha")
-    if out is None:
-        out = torch.empty((T, d.N), dtype=dtype, device=x.device)
-    code = _real(out.dtype, "out")
-    _shaped(_dev(out, out.dtype, "out"), (T, d.N), "out")
-    workspace, n = _workspace(workspace, bnn_experts_sum_workspace_size(d), x.device)
+    dtype = dtype if out is None else out.dtype
+    code = _real(dtype, "out")
+    out = _output(out, x, (T, d.N), dtype, "out")
+    workspace, n = _workspace(workspace, bnn_experts_sum_workspace_size(d), x)
     _check(lib.bnn_experts_sum(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(ids), _ptr(weights),
                                _ptr(offsets), _ptr(order), _ptr(alpha), code, _ptr(out),
                                _ptr(workspace), n, _stream(stream)))
@@ -730,11 +727,11 @@ def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=N
     _shaped(_dev(scale, torch.float32, "scale"), (L,), "scale")
     _shaped(_dev(alpha, torch.float32, "alpha"), (N,), "alpha")
     _shaped(_dev(offset, torch.float32, "offset"), (K,), "offset")
-    if out is None:
-        out = torch.empty((M, N), dtype=kind if dtype is None else dtype, device=x.device)
-    _shaped(_dev(out, out.dtype, "out"), (M, N), "out")
-    d = LoraDesc(M, N, K, L, rank, code, _real(out.dtype, "out"))
-    workspace, n = _workspace(workspace, bnn_bgemm_lora_workspace_size(d), x.device)
+    dtype = out.dtype if out is not None else kind if dtype is None else dtype
+    out_code = _real(dtype, "out")
+    out = _output(out, x, (M, N), dtype, "out")
+    d = LoraDesc(M, N, K, L, rank, code, out_code)
+    workspace, n = _workspace(workspace, bnn_bgemm_lora_workspace_size(d), x)
     _check(lib.bnn_bgemm_lora(ctypes.byref(d), _ptr(x), stride, _ptr(offset), _ptr(w),
                               _ptr(alpha), _ptr(ids), _ptr(a), _ptr(b), _ptr(scale), _ptr(order),
                               _ptr(out), _ptr(workspace), n, _stream(stream)))

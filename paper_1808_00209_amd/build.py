@@ -23,7 +23,7 @@ SOURCES = ["pack.hip", "bconv_valu.hip", "bconv_mfma.hip", "bconv_tile.hip", "bc
            "bconv_patch.hip", "fconv.hip", "fconv_bconv.hip", "bconv_bconv.hip", "bfc_chain.hip",
            "bfc_pair.hip", "bfc_gemm.hip", "bfc_tile.hip", "route.hip", "group_rows.hip",
            "experts.hip", "experts_tile.hip", "experts_skinny.hip",
-           "experts_combine.hip",
+           "experts_combine.hip", "experts_sum_rows.hip",
            "lora.hip", "lora_tile.hip", "lora_skinny.hip", "api.cpp", "experts_api.cpp"]
 ARCH = os.environ.get("BNN_OFFLOAD_ARCH", "gfx950")
 

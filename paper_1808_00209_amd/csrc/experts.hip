@@ -96,12 +96,26 @@ hipError_t launch_experts_fc(const ExpertsArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+namespace {
+
+// Few rows: every row reads its experts' weights by itself, up to 32 MiB of
+// them in all (one launch; rows x 8 of 64 experts, 4096 -> 1024, against
+// products and combine: 4 rows 6.0 and 13.1 us, 8 8.1 and 20.0, 32 28.5 and 21.3;
+// 32 rows 1024 -> 1024 13.4 and 12.9).
+bool few_rows(int64_t M, int32_t N, int32_t K) {
+  return M * N * words_of(K) <= (int64_t{8} << 20);
+}
+
+}  // namespace
+
 // The counts of every pair.
 size_t experts_sum_workspace(const bnn_experts_desc& d) {
-  return static_cast<size_t>(d.T) * d.top_k * d.N * sizeof(uint16_t);
+  const int64_t M = d.T * d.top_k;
+  return few_rows(M, d.N, d.K) ? 0 : static_cast<size_t>(M) * counts_stride(d.N) * sizeof(uint16_t);
 }
 
 hipError_t launch_experts_sum(const ExpertsArgs& a, hipStream_t s) {
+  if (use_tiles(a) && few_rows(a.M, a.N, a.K)) return launch_experts_sum_rows(a, s);
   if (use_tiles(a)) {
     uint16_t* counts = static_cast<uint16_t*>(a.ws);
     const hipError_t err = launch_products(a, counts, s);

@@ -39,11 +39,15 @@ struct ExpertsArgs {
 hipError_t launch_experts_fc(const ExpertsArgs& a, hipStream_t s);
 
 // The experts' products on the matrix cores (experts_tile.hip): bits, or with
-// counts [M][N] the numbers of equal bits (S + K) / 2.  x of at most 4 GiB.
+// counts [M][counts_stride(N)] the numbers of equal bits (S + K) / 2.  x of at most 4 GiB.
 bool experts_tile_supported(const ExpertsArgs& a);
 hipError_t launch_experts_tile(const ExpertsArgs& a, uint16_t* counts, hipStream_t s);
 // The same for few rows per expert (experts_skinny.hip).
 hipError_t launch_experts_skinny(const ExpertsArgs& a, uint16_t* counts, hipStream_t s);
+// Outputs from one row of counts to the next: N rounded up to 16 bytes.
+inline __host__ __device__ int32_t counts_stride(int32_t N) { return (N + 7) / 8 * 8; }
+// bnn_experts_sum for few rows in one launch (experts_sum_rows.hip).
+hipError_t launch_experts_sum_rows(const ExpertsArgs& a, hipStream_t s);
 // y from the counts (experts_combine.hip).
 hipError_t launch_experts_combine(const ExpertsArgs& a, const uint16_t* counts, hipStream_t s);
 

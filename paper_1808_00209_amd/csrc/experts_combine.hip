@@ -22,23 +22,9 @@ constexpr int kTokens = kNT / kColThreads;
 constexpr int kAhead = 8;            // pairs in flight
 constexpr size_t kMaxAlpha = 64 << 10;
 
-// 8 outputs from n on of `row` (WIDE: N is a multiple of 8).
-template <bool WIDE>
-__device__ __forceinline__ uint4 load_counts(const uint16_t* row, int n, int N) {
-  if constexpr (WIDE) {
-    return *reinterpret_cast<const uint4*>(row + n);
-  } else {
-    uint32_t v[4] = {};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (n + i < N) v[i / 2] |= static_cast<uint32_t>(row[n + i]) << (16 * (i & 1));
-    return uint4{v[0], v[1], v[2], v[3]};
-  }
-}
-
-template <bool WIDE>
+// alpha of 8 outputs from n on.
 __device__ __forceinline__ void load_alpha(const float* row, int n, int N, float (&f)[8]) {
-  if constexpr (WIDE) {
+  if (n + 8 <= N) {
     __builtin_memcpy(f, row + n, sizeof(f));
   } else {
 #pragma unroll
@@ -56,13 +42,13 @@ __device__ __forceinline__ void add_pair(float (&y)[8], const uint4& c, const fl
   }
 }
 
-template <class Y, bool WIDE>
+template <class Y>
 __device__ __forceinline__ void store_outputs(Y* row, int n, int N, const float (&y)[8]) {
   Y out[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) out[i] = from_f32<Y>(y[i]);
-  if constexpr (WIDE) {
-    __builtin_memcpy(__builtin_assume_aligned(row + n, 16), out, sizeof(out));
+  if (n + 8 <= N) {
+    __builtin_memcpy(row + n, out, sizeof(out));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -72,7 +58,7 @@ __device__ __forceinline__ void store_outputs(Y* row, int n, int N, const float 
 
 // STAGED: block (256 outputs, a range of rows), alphas in LDS; else block
 // (row, 8 blockDim outputs).
-template <class Y, bool WIDE, bool STAGED>
+template <class Y, bool STAGED>
 __global__ __launch_bounds__(kNT) void experts_combine_kernel(ExpertsArgs a,
                                                               const uint16_t* __restrict__ counts,
                                                               int rows) {
@@ -85,7 +71,7 @@ __global__ __launch_bounds__(kNT) void experts_combine_kernel(ExpertsArgs a,
       const int e = v / kColThreads, col = 8 * (v % kColThreads);
       float f[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
       if (a.alpha && n0 + col < a.N)
-        load_alpha<WIDE>(a.alpha + static_cast<size_t>(e) * a.N, n0 + col, a.N, f);
+        load_alpha(a.alpha + static_cast<size_t>(e) * a.N, n0 + col, a.N, f);
       __builtin_memcpy(__builtin_assume_aligned(alphas + e * kCols + col, 16), f, sizeof(f));
     }
     __syncthreads();
@@ -100,6 +86,7 @@ __global__ __launch_bounds__(kNT) void experts_combine_kernel(ExpertsArgs a,
     n = 8 * (blockIdx.y * static_cast<int>(blockDim.x) + tid);
   }
   if (n >= a.N) return;
+  const int ns = counts_stride(a.N);
   for (; t < end; t += step) {
     float y[8] = {};
     for (int j0 = 0; j0 < a.top_k; j0 += kAhead) {
@@ -118,11 +105,12 @@ __global__ __launch_bounds__(kNT) void experts_combine_kernel(ExpertsArgs a,
         const bool in = id[j] >= 0 && id[j] < a.E;
         if (!in) id[j] = -1;
         const int m = t * a.top_k + min(j0 + j, a.top_k - 1);
-        if (in) c[j] = load_counts<WIDE>(counts + static_cast<size_t>(m) * a.N, n, a.N);
+        if (in)
+          c[j] = *reinterpret_cast<const uint4*>(counts + static_cast<size_t>(m) * ns + n);
         if constexpr (!STAGED) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) f[j][i] = 1.0f;
-          if (in && a.alpha) load_alpha<WIDE>(a.alpha + static_cast<size_t>(id[j]) * a.N, n, a.N, f[j]);
+          if (in && a.alpha) load_alpha(a.alpha + static_cast<size_t>(id[j]) * a.N, n, a.N, f[j]);
         }
       }
 #pragma unroll
@@ -139,11 +127,11 @@ __global__ __launch_bounds__(kNT) void experts_combine_kernel(ExpertsArgs a,
         }
       }
     }
-    store_outputs<Y, WIDE>(static_cast<Y*>(a.y) + static_cast<size_t>(t) * a.N, n, a.N, y);
+    store_outputs<Y>(static_cast<Y*>(a.y) + static_cast<size_t>(t) * a.N, n, a.N, y);
   }
 }
 
-template <class Y, bool WIDE>
+template <class Y>
 void launch_typed(const ExpertsArgs& a, const uint16_t* counts, hipStream_t s) {
   const size_t lds = static_cast<size_t>(a.E) * kCols * sizeof(float);
   const int cols = (a.N + kCols - 1) / kCols;
@@ -152,24 +140,19 @@ void launch_typed(const ExpertsArgs& a, const uint16_t* counts, hipStream_t s) {
   const int rows = static_cast<int>((a.T * cols + 511) / 512);
   if (lds <= kMaxAlpha && rows >= 64) {
     const dim3 grid(static_cast<unsigned>(cols), static_cast<unsigned>((a.T + rows - 1) / rows));
-    experts_combine_kernel<Y, WIDE, true><<<grid, kNT, lds, s>>>(a, counts, rows);
+    experts_combine_kernel<Y, true><<<grid, kNT, lds, s>>>(a, counts, rows);
   } else {
     const int threads = a.N >= 8 * kNT ? kNT : ((a.N + 7) / 8 + 63) / 64 * 64;
     const dim3 grid(static_cast<unsigned>(a.T),
                     static_cast<unsigned>((a.N + 8 * threads - 1) / (8 * threads)));
-    experts_combine_kernel<Y, WIDE, false><<<grid, threads, 0, s>>>(a, counts, 1);
+    experts_combine_kernel<Y, false><<<grid, threads, 0, s>>>(a, counts, 1);
   }
 }
 
 }  // namespace
 
 hipError_t launch_experts_combine(const ExpertsArgs& a, const uint16_t* counts, hipStream_t s) {
-  with_real_type(a.dtype, [&](auto v) {
-    if (a.N % 8 == 0)
-      launch_typed<decltype(v), true>(a, counts, s);
-    else
-      launch_typed<decltype(v), false>(a, counts, s);
-  });
+  with_real_type(a.dtype, [&](auto v) { launch_typed<decltype(v)>(a, counts, s); });
   return hipGetLastError();
 }
 

@@ -73,21 +73,16 @@ __global__ __launch_bounds__(64 * NW) void experts_skinny_kernel(EsArgs a) {
     if (c >= rows) return;
     // Register e holds output 8 (e / 4) + 4 h + e % 4 of row c.
     const float half = 0.5f * static_cast<float>(a.K);
-    uint16_t* dst = a.counts + static_cast<size_t>(pair) * a.N + n0;
+    const int ns = counts_stride(a.N);
+    uint16_t* dst = a.counts + static_cast<size_t>(pair) * ns + n0;
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
       const int n = 2 * e + 4 * h;
       uint32_t v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = static_cast<uint32_t>(0.5f * acc[e + i] + half);
-      if ((a.N & 3) == 0) {
-        if (n0 + n < a.N)
-          *reinterpret_cast<uint2*>(dst + n) = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (n0 + n + i < a.N) dst[n + i] = static_cast<uint16_t>(v[i]);
-      }
+      if (n0 + n < ns)
+        *reinterpret_cast<uint2*>(dst + n) = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
     }
   } else {
 #pragma unroll

@@ -117,15 +117,9 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
         const int m = __shfl(pair[pt], row);
         const uint4 v = *reinterpret_cast<const uint4*>(&ts[row * kCountStride + 8 * (lane & 7)]);
         if ((t.wpi * PT + pt) * 32 + row < rows) {
-          uint16_t* dst = a.counts + static_cast<size_t>(m) * a.N + f;
-          if ((a.N & 7) == 0) {
-            if (f < a.N) *reinterpret_cast<uint4*>(dst) = v;
-          } else {
-            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (f + i < a.N) dst[i] = static_cast<uint16_t>(u[i / 2] >> (16 * (i & 1)));
-          }
+          const int ns = counts_stride(a.N);
+          if (f < ns)
+            *reinterpret_cast<uint4*>(a.counts + static_cast<size_t>(m) * ns + f) = v;
         }
       }
     }
