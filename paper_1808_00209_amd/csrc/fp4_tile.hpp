@@ -104,8 +104,13 @@ __device__ __forceinline__ void tile_loop(v16f (&acc)[2][PT], v4i* act, const Ti
   int abase[PT];
 #pragma unroll
   for (int pt = 0; pt < PT; ++pt) abase[pt] = ((t.wpi * PT + pt) * 32 + c) * kTilePS + 4 * h;
+  if (whole > 0) {
 #pragma unroll
-  for (int s = 0; s < kTileKS; ++s) stage_word(xr[0], 0, s, 0, std::true_type{});
+    for (int s = 0; s < kTileKS; ++s) stage_word(xr[0], 0, s, 0, std::false_type{});
+  } else {
+#pragma unroll
+    for (int s = 0; s < kTileKS; ++s) stage_word(xr[0], 0, s, 0, std::true_type{});
+  }
   load_x(0, min(kRing, nch - 1));
   __syncthreads();
 
@@ -175,7 +180,10 @@ __device__ __forceinline__ void tile_loop(v16f (&acc)[2][PT], v4i* act, const Ti
     }
   };
   int ch = 0;
-  for (; ch + kRing < whole; ch += kRing) trip(ch, std::false_type{});
+  // (with K in whole chunks nothing is masked: what the last chunk stages is
+  // read by no one)
+  const int plain = whole == nch ? nch - kRing : whole - kRing - 1;
+  for (; ch <= plain; ch += kRing) trip(ch, std::false_type{});
   for (; ch < nch; ch += kRing) trip(ch, std::true_type{});
 }
 
