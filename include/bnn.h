@@ -575,7 +575,8 @@ typedef struct bnn_experts_desc {
  *   offsets, order   of bnn_group_rows over the T * top_k ids.  Entries out of
  *            range are clamped into it, so that no access leaves the buffers.
  *   out_bits [T * top_k][ceil(N / 32)] u32.
- * T >= 0 (0 launches nothing), T * top_k < 2^24, N <= 65536, K <= 65535.
+ * T >= 0 (0 launches nothing), T * top_k < 2^24, N <= 65536, K <= 65535, and
+ * T * top_k * ceil(N / 64) <= 2^28.
  * x, w and out_bits 16-byte aligned.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE,
  * BNN_ERR_ALIGN, BNN_ERR_HIP.
  */
@@ -643,8 +644,8 @@ typedef struct bnn_lora_desc {
  *            of range are clamped into it.
  *   y        [M][N].
  *   workspace as for bnn_experts_sum.
- * M >= 0 (0 launches nothing), M < 2^24, N <= 65536, K <= 65536.  x, w, a, b
- * and y 16-byte aligned.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN,
+ * M >= 0 (0 launches nothing), M < 2^24, N <= 65536, K <= 65536, M * ceil(N /
+ * 64) <= 2^28.  x, w, a, b and y 16-byte aligned.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN,
  * BNN_ERR_UNSUPPORTED (rank), BNN_ERR_WORKSPACE, BNN_ERR_HIP.
  */
 bnn_status bnn_bgemm_lora_workspace_size(const bnn_lora_desc* d, size_t* bytes);

@@ -16,6 +16,8 @@ using bnn::hip_status;
 using bnn::ok;
 
 constexpr int64_t kMaxRows = int64_t{1} << 24;
+// Rows times 64-output tiles: a grid's work-items stay below 2^32.
+constexpr int64_t kMaxTiles = int64_t{1} << 28;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -73,6 +75,9 @@ bnn_status experts_check(const bnn_experts_desc* d, const char* what) {
     return fail(BNN_ERR_SHAPE, "%s: share %d, not 0 or 1", what, d->share);
   if (d->T < 0 || d->T >= kMaxRows || d->T * d->top_k >= kMaxRows)
     return fail(BNN_ERR_SHAPE, "%s: %lld rows of %d experts", what, (long long)d->T, d->top_k);
+  if (d->T * d->top_k * ((d->N + 63) / 64) > kMaxTiles)
+    return fail(BNN_ERR_SHAPE, "%s: %lld rows of %d outputs are too large for one launch", what,
+                (long long)(d->T * d->top_k), d->N);
   return BNN_OK;
 }
 
@@ -99,6 +104,9 @@ bnn_status lora_check(const bnn_lora_desc* d) {
     return fail(BNN_ERR_SHAPE, "lora: M=%lld rows", (long long)d->M);
   if (d->N < 1 || d->N > 65536 || d->K < 1 || d->K > 65536)
     return fail(BNN_ERR_SHAPE, "lora: N=%d K=%d out of range", d->N, d->K);
+  if (d->M * ((d->N + 63) / 64) > kMaxTiles)
+    return fail(BNN_ERR_SHAPE, "lora: %lld rows of %d outputs are too large for one launch",
+                (long long)d->M, d->N);
   if (d->adapters < 1 || d->adapters > BNN_MAX_EXPERTS)
     return fail(BNN_ERR_SHAPE, "lora: %d adapters, not in 1..%d", d->adapters, BNN_MAX_EXPERTS);
   if (d->rank < 1) return fail(BNN_ERR_SHAPE, "lora: rank %d < 1", d->rank);

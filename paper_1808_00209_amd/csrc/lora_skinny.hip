@@ -16,7 +16,7 @@ namespace {
 // ------------------------------------------------------------ x -> bits, u ---
 constexpr int kNT = 256;
 constexpr int kNW = kNT / 64;
-constexpr int kAhead = 4;  // 512-element pieces in flight
+constexpr int kAdapters = 4;  // adapters whose rows of b are in flight
 
 // 8 elements from p on, of which `left` exist (the others read 0).
 template <class T>
@@ -39,18 +39,29 @@ __global__ __launch_bounds__(kNT) void lora_down_rows_kernel(LoraArgs a, float* 
   if (r >= a.rank) return;
   const int row = lora_row(a, p);
   const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+  constexpr int kAhead = 4;  // 512-element pieces in flight (eight: no quicker)
   if (job == 0) {
     const int kw = (a.K + 31) >> 5;
-    for (int k0 = 8 * lane; k0 < a.K + 8 * lane; k0 += 512) {  // (all lanes take part)
-      T v[8];
-      float off[8] = {};
-      load8(v, x + k0, a.K - k0);
-      if (a.offset) load8(off, a.offset + k0, a.K - k0);
-      uint32_t byte = 0;
+    for (int k0 = 0; k0 < a.K; k0 += 512 * kAhead) {
+      T v[kAhead][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) byte = 2 * byte + (to_f32(v[e]) + off[e] > 0.0f ? 1u : 0u);
-      const uint32_t word = or_quad(byte << (24 - 8 * (lane & 3)));
-      if ((lane & 3) == 0 && k0 < a.K) bits[static_cast<size_t>(p) * kw + k0 / 32] = word;
+      for (int i = 0; i < kAhead; ++i) {
+        const int k = k0 + 512 * i + 8 * lane;
+        if (k0 + 512 * i < a.K) load8(v[i], x + k, a.K - k);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (k0 + 512 * i >= a.K) break;  // (uniform: all lanes take part below)
+        const int k = k0 + 512 * i + 8 * lane;
+        float off[8] = {};
+        if (a.offset) load8(off, a.offset + k, a.K - k);
+        uint32_t byte = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          byte = 2 * byte + (to_f32(v[i][e]) + off[e] > 0.0f ? 1u : 0u);
+        const uint32_t word = or_quad(byte << (24 - 8 * (lane & 3)));
+        if ((lane & 3) == 0 && k < a.K) bits[static_cast<size_t>(p) * kw + k / 32] = word;
+      }
     }
     return;
   }
@@ -58,17 +69,22 @@ __global__ __launch_bounds__(kNT) void lora_down_rows_kernel(LoraArgs a, float* 
   if (l < 0) return;
   const T* w = static_cast<const T*>(a.a) + (static_cast<size_t>(l) * a.rank + r) * a.K;
   float sum = 0.0f;
-  for (int k0 = 8 * lane; k0 < a.K; k0 += 512 * kAhead) {
+  for (int k0 = 0; k0 < a.K; k0 += 512 * kAhead) {
     T xv[kAhead][8], wv[kAhead][8];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      load8(xv[i], x + k0 + 512 * i, a.K - k0 - 512 * i);
-      load8(wv[i], w + k0 + 512 * i, a.K - k0 - 512 * i);
+      const int k = k0 + 512 * i + 8 * lane;
+      if (k0 + 512 * i < a.K) {
+        load8(xv[i], x + k, a.K - k);
+        load8(wv[i], w + k, a.K - k);
+      }
     }
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
+    for (int i = 0; i < kAhead; ++i) {
+      if (k0 + 512 * i >= a.K) break;
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += to_f32(xv[i][e]) * to_f32(wv[i][e]);
+    }
   }
 #pragma unroll
   for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
@@ -105,51 +121,63 @@ __global__ __launch_bounds__(64 * NW) void lora_up_skinny_kernel(UsArgs g) {
   t.tmask = g.tmask;
   const int row = lora_row(a, p);
   const int id = p < a.M ? lora_adapter(a, row) : -1;
-  v16f acc = skinny_part<NW>(t, wave, h);
-
   // u b^T: 16 ranks of an adapter are a job of wave (adapter + ranks / 16) mod
-  // NW, so that a row's sums do not hang on the rows beside it.
-  v16f low = {};
+  // NW, so that a row's sums do not hang on the rows beside it.  The first
+  // jobs' values are loaded before the binary products.
   const uint32_t have = static_cast<uint32_t>(__ballot(id >= 0));
-  if (have) {
-    for (int r = 0; r < a.rank; r += 16) {
-      const int rr = r + 8 * h;
-      const bool in = rr < a.rank;
-      float v[8];
-      const float* src = g.u + (id >= 0 && in ? static_cast<size_t>(p) * a.rank + rr : size_t{0});
-      __builtin_memcpy(v, __builtin_assume_aligned(src, 16), sizeof(v));
-      for (int s = 1; s < g.slices; ++s) {
-        float w[8];
-        __builtin_memcpy(
-            w, __builtin_assume_aligned(src + static_cast<size_t>(s) * a.M * a.rank, 16),
-            sizeof(w));
+  float v[8];            // u, 16 ranks of the row
+  int l[kAdapters];
+  RawB<T> b[kAdapters];  // and of this output's rows of b
+  auto load_u = [&](int r) {
+    const int rr = r + 8 * h;
+    const float* src =
+        g.u + (id >= 0 && rr < a.rank ? static_cast<size_t>(p) * a.rank + rr : size_t{0});
+    __builtin_memcpy(v, __builtin_assume_aligned(src, 16), sizeof(v));
+    for (int s = 1; s < g.slices; ++s) {
+      float w[8];
+      __builtin_memcpy(
+          w, __builtin_assume_aligned(src + static_cast<size_t>(s) * a.M * a.rank, 16), sizeof(w));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += w[e];
-      }
-      for (uint32_t todo = have; todo;) {
-        // Up to kAhead of this wave's adapters at a time, their rows of b in flight.
-        int l[kAhead];
-        RawB<T> b[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          l[i] = -1;
-          while (todo && l[i] < 0) {
-            const int q = __builtin_amdgcn_readlane(id, __builtin_ctz(todo));
-            todo &= ~static_cast<uint32_t>(__ballot(id == q));
-            if (((q + (r >> 4)) & (NW - 1)) == wave) l[i] = q;
-          }
-          if (l[i] >= 0) b[i] = load_b<T>(a, l[i], n0 + c, rr);
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          if (l[i] < 0) continue;
-          v8bf bf[kParts<T>], uf[3];
-          split_b<T>(b[i], in && n0 + c < a.N, bf);
-          split_frag<3>(v, in && id == l[i], uf);
-          add_parts<T>(low, bf, uf);
-        }
-      }
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
     }
+  };
+  // This wave's next adapters among `todo` for ranks r .., their rows of b.
+  auto load_adapters = [&](uint32_t& todo, int r) {
+#pragma unroll
+    for (int i = 0; i < kAdapters; ++i) {
+      l[i] = -1;
+      while (todo && l[i] < 0) {
+        const int q = __builtin_amdgcn_readlane(id, __builtin_ctz(todo));
+        todo &= ~static_cast<uint32_t>(__ballot(id == q));
+        if (((q + (r >> 4)) & (NW - 1)) == wave) l[i] = q;
+      }
+      if (l[i] >= 0) b[i] = load_b<T>(a, l[i], n0 + c, r + 8 * h);
+    }
+  };
+  uint32_t todo = have;
+  if (have) {
+    load_u(0);
+    load_adapters(todo, 0);
+  }
+  v16f acc = skinny_part<NW>(t, wave, h);
+  v16f low = {};
+  for (int r = 0; have && r < a.rank;) {
+    const bool in = r + 8 * h < a.rank;
+#pragma unroll
+    for (int i = 0; i < kAdapters; ++i) {
+      if (l[i] < 0) continue;
+      v8bf bf[kParts<T>], uf[3];
+      split_b<T>(b[i], in && n0 + c < a.N, bf);
+      split_frag<3>(v, in && id == l[i], uf);
+      add_parts<T>(low, bf, uf);
+    }
+    if (!todo) {
+      r += 16;
+      if (r >= a.rank) break;
+      todo = have;
+      load_u(r);
+    }
+    load_adapters(todo, r);
   }
   skinny_join<NW>(acc, part, wave, lane);
   if (have) skinny_join<NW>(low, low_part, wave, lane);

@@ -83,7 +83,8 @@ def _experts_desc(**kw):
 
 
 BAD_EXPERTS = [dict(E=0), dict(E=1025), dict(top_k=0), dict(top_k=17), dict(N=0), dict(K=0),
-               dict(N=65537), dict(K=65536), dict(share=2), dict(T=-1), dict(T=1 << 23)]
+               dict(N=65537), dict(K=65536), dict(share=2), dict(T=-1), dict(T=1 << 23),
+               dict(T=1 << 20, N=65536)]
 
 
 @pytest.mark.parametrize("kw", BAD_EXPERTS, ids=str)
@@ -137,7 +138,7 @@ def _lora_desc(**kw):
     (dict(M=-1), "SHAPE"), (dict(M=1 << 24), "SHAPE"), (dict(N=0), "SHAPE"), (dict(N=65537), "SHAPE"),
     (dict(K=0), "SHAPE"), (dict(K=65537), "SHAPE"), (dict(adapters=0), "SHAPE"),
     (dict(adapters=1025), "SHAPE"), (dict(rank=0), "SHAPE"), (dict(rank=12), "UNSUPPORTED"),
-    (dict(rank=264), "UNSUPPORTED"), (dict(dtype=3), "SHAPE"), (dict(out_dtype=3), "SHAPE")], ids=str)
+    (dict(M=1 << 22, N=65536), "SHAPE"), (dict(rank=264), "UNSUPPORTED"), (dict(dtype=3), "SHAPE"), (dict(out_dtype=3), "SHAPE")], ids=str)
 def test_lora_descriptor(lib, kw, status):
     d, n = _lora_desc(**kw), ctypes.c_size_t()
     _refused(lib.bnn_bgemm_lora(ctypes.byref(d), P, 1 << 20, None, P, None, P, P, P, None, None, P, P,

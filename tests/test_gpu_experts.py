@@ -22,6 +22,15 @@ CASES = [
     (33, 3, 3, 1023, 32, 0.0), (16, 6, 12, 8192, 48, 0.0), (1030, 1, 5, 96, 65, 0.01),
     (1500, 2, 4, 288, 700, 0.02),
 ]
+# Sums that take the products and the combining pass (over 32 MiB of weight
+# rows read): few long rows in the skinny tiles, whole tiles of every shape
+# (64, 128 and 256 outputs; 32, 64 and 128 rows), alphas staged in LDS.
+LARGE = [
+    (300, 2, 3, 8192, 100, 0.1), (40, 4, 40, 16384, 130, 0.0), (20, 16, 70, 65535, 33, 0.1),
+    (1500, 2, 4, 1000, 700, 0.02), (2000, 2, 5, 4097, 60, 0.0), (900, 3, 30, 1023, 515, 0.05),
+    (3000, 1, 2, 700, 300, 0.0), (700, 4, 50, 640, 1030, 0.0), (33000, 1, 9, 33, 257, 0.02),
+    (5000, 8, 64, 64, 1001, 0.01), (1, 16, 900, 4095, 5000, 0.0),
+]
 
 
 def _ids(g, T, k, E, none):
@@ -49,7 +58,7 @@ def _dev(*arrays):
 
 
 @pytest.mark.parametrize("per_pair", [False, True])
-@pytest.mark.parametrize("case", CASES, ids=str)
+@pytest.mark.parametrize("case", CASES + LARGE[:8], ids=str)
 def test_experts_fc(case, per_pair):
     T, k, E, K, N, none = case
     g = np.random.default_rng(T + K + N)
@@ -69,10 +78,22 @@ def test_experts_fc(case, per_pair):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16], ids=str)
 @pytest.mark.parametrize("case", CASES, ids=str)
 def test_experts_sum(case, dtype):
+    _sum(case, dtype, ((True, True), (False, False)))
+
+
+@pytest.mark.parametrize("case", LARGE, ids=str)
+def test_experts_sum_of_many_products(case):
+    T, k, E, K, N, _ = case
+    assert bnn.bnn_experts_sum_workspace_size(bnn.ExpertsDesc(T, k, E, N, K, 0)) > 0
+    i = LARGE.index(case)
+    _sum(case, [torch.float32, torch.bfloat16, torch.float16][i % 3], ((i % 2 == 0, True),))
+
+
+def _sum(case, dtype, forms):
     T, k, E, K, N, none = case
     g = np.random.default_rng(T + K + N + 1)
     ids = _ids(g, T, k, E, none)
-    for per_pair, scaled in ((True, True), (False, False)):
+    for per_pair, scaled in forms:
         x, w = _words(g, T * k if per_pair else T, bnn.words(K)), _words(g, E, N, bnn.words(K))
         weights = g.random((T, k)).astype(np.float32) - 0.25
         weights[ids < 0] = np.nan  # is not read

@@ -27,6 +27,12 @@ CASES = [
     (129, 512, 128, 3, 128, "fp16", "bf16"), (300, 777, 65, 9, 8, "fp16", "fp32"),
     (515, 256, 513, 30, 16, "bf16", "fp32"), (1200, 192, 300, 4, 64, "fp32", "fp32"),
     (260, 4100, 40, 2, 16, "bf16", "bf16"), (2050, 72, 70, 1000, 8, "bf16", "fp16"),
+    # many rows: x in one pass on the matrix cores, 16, 32 and 64 ranks at a
+    # time, k in slices; large tiles of every shape
+    (4100, 300, 515, 6, 8, "bf16", "fp32"), (1100, 2100, 90, 3, 24, "fp16", "fp16"),
+    (500, 1029, 700, 4, 40, "bf16", "bf16"), (300, 1500, 300, 9, 136, "fp16", "fp32"),
+    (1030, 643, 1100, 2, 16, "fp32", "fp32"), (200, 1000, 130, 70, 256, "fp32", "bf16"),
+    (5000, 256, 64, 500, 16, "bf16", "bf16"), (3000, 512, 2050, 1, 64, "bf16", "bf16"),
 ]
 
 
