@@ -1,5 +1,6 @@
-// The shape of the fp4_tile.hpp tiles that the experts' and adapters' kernels
-// cut their work into.  A pure function of the sizes, on the host.
+// Which kernels the experts' and adapters' calls take and how these cut their
+// work.  Pure functions of the sizes, on the host, so that a choice can be
+// looked at without a GPU.
 #pragma once
 
 #include <stdint.h>
@@ -44,6 +45,81 @@ TileShape tile_shape(int64_t N, int64_t chunks, double fixed, double tail, F row
       }
     }
   return best;
+}
+
+// ---------------------------------------------------------------- experts ---
+
+// bnn_experts_sum for few rows: every row reads its experts' weights by itself,
+// up to 32 MiB of them in all (experts_sum_rows.hip, one launch; rows x 8 of 64
+// experts, 4096 -> 1024, against products and combining pass: 4 rows 6.0 and
+// 13.1 us, 8 8.1 and 20.0, 32 28.5 and 21.3; 32 rows 1024 -> 1024 13.4 and 12.9).
+inline bool experts_sum_by_rows(int64_t M, int64_t N, int64_t K) {
+  return M * N * ((K + 31) / 32) <= (int64_t{8} << 20);
+}
+
+// The skinny kernel (experts_skinny.hip) has a workgroup per 32 rows of an
+// expert and 32 outputs and splits K over its waves: quicker while the whole
+// chip takes about one round of them, several times slower at many (skinny
+// against tile kernel, rows x experts per row of E, K -> N: 1 x 8 of 64, 1024 ->
+// 4096: 5.7 and 6.4 us, 4 x 8: 12.1 and 8.7; 4 x 8, 4096 -> 1024: 8.3 and 10.7, 64 x
+// 8: 19.2 and 11.4; 1 of 4, 4096 -> 4096: 4.6 and 10.6; 1000 x 2 of 8, 512 -> 512:
+// 4.5 and 5.7; 301 x 3 of 24, 1000 -> 1500: 10.3 and 6.9).
+inline bool experts_skinny(int64_t M, int64_t E, int64_t N) {
+  return ((M + 31) / 32 + (E < M ? E : M)) * ((N + 31) / 32) <= 1200;
+}
+
+// Tiles of experts_tile.hip.  Row tiles: the whole ones and, for every expert
+// that has rows, half a tile.
+inline TileShape experts_shape(int64_t M, int64_t E, int64_t N, int64_t chunks) {
+  const double some = static_cast<double>(E < M ? E : M);
+  return tile_shape(N, chunks, 10000, 500, [&](int rows) {
+    return static_cast<double>(M) / rows + some / 2 + (some < 2 ? 0.5 : 0.0);
+  });
+}
+
+// The combining pass (experts_combine.hip) stages the alphas of all experts for
+// 256 outputs in LDS (at most 64 KiB of them) where a block, two per compute
+// unit, has 64 rows or more: fewer do not pay for the staging.  Rows per block,
+// or 0 for the form that reads them as it goes.
+constexpr int kCombineCols = 256;
+inline int combine_rows(int64_t T, int64_t E, int64_t N) {
+  const int64_t cols = (N + kCombineCols - 1) / kCombineCols;
+  const int64_t rows = (T * cols + 511) / 512;
+  return E * kCombineCols * 4 <= (64 << 10) && rows >= 64 ? static_cast<int>(rows) : 0;
+}
+
+// ------------------------------------------------------------- with adapters ---
+
+// A wave per row and rank component (lora_skinny.hip) while all of them are
+// few rounds of the chip (both steps, rows and then k tiles, in us: 32 rows x
+// 4096, rank 16, 28 adapters 14.2 and 38.1; 777 x 1100, rank 8 17.1 and 24.8; 512 x
+// 4096, rank 16 23.5 and 26.3; 1024 x 4096, rank 16 27.4 and 24.6; 4096 x 1024,
+// rank 8 28.2 and 20.7).
+inline bool lora_down_by_rows(int64_t M, int64_t rank) { return M * (rank + 1) <= 16384; }
+
+// Otherwise k slices of the down pass of lora_tile.hip (blocks of 32 rows and 8
+// waves): a block per compute unit (two: 37 against 34 us for 8192 rows of
+// 4096), at least one group of 128 k for every wave.
+inline int lora_down_slices(int64_t M, int64_t K, int64_t rank) {
+  if (M < 1 || lora_down_by_rows(M, rank)) return 1;
+  const int64_t blocks = (M + 31) / 32 * ((rank + 63) / 64);
+  const int64_t most = (K + 1023) / 1024;
+  const int64_t want = (256 + blocks - 1) / blocks;
+  return static_cast<int>(want < most ? want : most);
+}
+
+// K split over a workgroup per 32 x 32 tile (lora_skinny.hip) while they are
+// about three per compute unit (128 rows, 4096 -> 4096, many adapters 18.7 us,
+// in the larger tiles 33.6; one per 16 rows, rank 64 21.8 and 25.5; 256 rows 27.1
+// and 26.6).
+inline bool lora_up_skinny(int64_t M, int64_t N) {
+  return (M + 31) / 32 * ((N + 31) / 32) <= 800;
+}
+
+inline TileShape lora_shape(int64_t M, int64_t N, int64_t chunks) {
+  return tile_shape(N, chunks, 7000, 2500, [&](int rows) {
+    return static_cast<double>((M + rows - 1) / rows);
+  });
 }
 
 }  // namespace bnn

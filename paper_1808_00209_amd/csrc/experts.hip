@@ -2,6 +2,7 @@
 // kernel, the vector-ALU kernels (a thread per output, XOR + popcount over the
 // row's words, Eq. 4; option algo = BNN_ALGO_VALU and rows of over 4 GiB).
 #include "dtypes.hpp"
+#include "expert_plans.hpp"
 #include "experts.hpp"
 #include "kernels.hpp"
 
@@ -74,16 +75,8 @@ bool use_tiles(const ExpertsArgs& a) {
   return options().algo != BNN_ALGO_VALU && experts_tile_supported(a);
 }
 
-// The skinny kernel has a workgroup per 32 rows of an expert and 32 outputs,
-// and splits K over its waves: quicker while the whole chip takes about one
-// round of them, several times slower at many (measured, skinny against tile
-// kernel, rows x experts per row of E, K -> N: 1 x 8 of 64, 1024 -> 4096: 5.7
-// and 6.4 us, 4 x 8: 12.1 and 8.7; 4 x 8, 4096 -> 1024: 8.3 and 10.7, 64 x 8: 19.2
-// and 11.4; 1 of 4, 4096 -> 4096: 4.6 and 10.6; 1000 x 2 of 8, 512 -> 512: 4.5 and
-// 5.7; 301 x 3 of 24, 1000 -> 1500: 10.3 and 6.9).
 hipError_t launch_products(const ExpertsArgs& a, uint16_t* counts, hipStream_t s) {
-  const int64_t tiles = (a.M + 31) / 32 + (a.E < a.M ? a.E : a.M);
-  return tiles * words_of(a.N) <= 1200 ? launch_experts_skinny(a, counts, s)
+  return experts_skinny(a.M, a.E, a.N) ? launch_experts_skinny(a, counts, s)
                                        : launch_experts_tile(a, counts, s);
 }
 
@@ -96,26 +89,14 @@ hipError_t launch_experts_fc(const ExpertsArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-namespace {
-
-// Few rows: every row reads its experts' weights by itself, up to 32 MiB of
-// them in all (one launch; rows x 8 of 64 experts, 4096 -> 1024, against
-// products and combine: 4 rows 6.0 and 13.1 us, 8 8.1 and 20.0, 32 28.5 and 21.3;
-// 32 rows 1024 -> 1024 13.4 and 12.9).
-bool few_rows(int64_t M, int32_t N, int32_t K) {
-  return M * N * words_of(K) <= (int64_t{8} << 20);
-}
-
-}  // namespace
-
 // The counts of every pair.
 size_t experts_sum_workspace(const bnn_experts_desc& d) {
   const int64_t M = d.T * d.top_k;
-  return few_rows(M, d.N, d.K) ? 0 : static_cast<size_t>(M) * counts_stride(d.N) * sizeof(uint16_t);
+  return experts_sum_by_rows(M, d.N, d.K) ? 0 : static_cast<size_t>(M) * counts_stride(d.N) * sizeof(uint16_t);
 }
 
 hipError_t launch_experts_sum(const ExpertsArgs& a, hipStream_t s) {
-  if (use_tiles(a) && few_rows(a.M, a.N, a.K)) return launch_experts_sum_rows(a, s);
+  if (use_tiles(a) && experts_sum_by_rows(a.M, a.N, a.K)) return launch_experts_sum_rows(a, s);
   if (use_tiles(a)) {
     uint16_t* counts = static_cast<uint16_t*>(a.ws);
     const hipError_t err = launch_products(a, counts, s);

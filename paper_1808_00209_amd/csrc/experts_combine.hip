@@ -10,17 +10,17 @@
 // with one read after another.  Many rows therefore stage the alphas of all
 // experts for 256 outputs in LDS; few have all their reads in flight.
 #include "dtypes.hpp"
+#include "expert_plans.hpp"
 #include "experts.hpp"
 
 namespace bnn {
 namespace {
 
 constexpr int kNT = 256;
-constexpr int kCols = 256;           // outputs per block of the staged form
+constexpr int kCols = kCombineCols;  // outputs per block of the staged form
 constexpr int kColThreads = kCols / 8;
 constexpr int kTokens = kNT / kColThreads;
 constexpr int kAhead = 8;            // pairs in flight
-constexpr size_t kMaxAlpha = 64 << 10;
 
 // alpha of 8 outputs from n on.
 __device__ __forceinline__ void load_alpha(const float* row, int n, int N, float (&f)[8]) {
@@ -133,12 +133,9 @@ __global__ __launch_bounds__(kNT) void experts_combine_kernel(ExpertsArgs a,
 
 template <class Y>
 void launch_typed(const ExpertsArgs& a, const uint16_t* counts, hipStream_t s) {
-  const size_t lds = static_cast<size_t>(a.E) * kCols * sizeof(float);
-  const int cols = (a.N + kCols - 1) / kCols;
-  // Staged from 64 rows per block on, with two blocks per compute unit: fewer
-  // rows do not pay for the staging.
-  const int rows = static_cast<int>((a.T * cols + 511) / 512);
-  if (lds <= kMaxAlpha && rows >= 64) {
+  if (const int rows = combine_rows(a.T, a.E, a.N)) {
+    const int cols = (a.N + kCols - 1) / kCols;
+    const size_t lds = static_cast<size_t>(a.E) * kCols * sizeof(float);
     const dim3 grid(static_cast<unsigned>(cols), static_cast<unsigned>((a.T + rows - 1) / rows));
     experts_combine_kernel<Y, true><<<grid, kNT, lds, s>>>(a, counts, rows);
   } else {

@@ -171,11 +171,7 @@ hipError_t launch_experts_tile(const ExpertsArgs& a, uint16_t* counts, hipStream
   e.share = a.share;
   e.x_bytes = static_cast<uint32_t>(static_cast<int64_t>(a.M / a.share) * e.Kw * 4);
   e.w_bytes = static_cast<uint32_t>(static_cast<int64_t>(a.N) * e.Kw * 4);
-  // Row tiles: the whole ones and, for every expert that has rows, half a tile.
-  const double some = a.E < a.M ? a.E : a.M;
-  const TileShape shape = tile_shape(a.N, e.chunks, 10000, 500, [&](int rows) {
-    return static_cast<double>(a.M) / rows + some / 2 + (some < 2 ? 0.5 : 0.0);
-  });
+  const TileShape shape = experts_shape(a.M, a.E, a.N, e.chunks);
   e.wfl = shape.wfl;
   const int rows = shape.rows();
   e.rlog = rows == 128 ? 7 : rows == 64 ? 6 : 5;

@@ -410,17 +410,8 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
   }
 }
 
-// k slices of the down pass: a block per compute unit (two: 37 against 34 us
-// for 8192 rows of 4096), at least one group of 128 k for every wave.
-int down_slices(int64_t M, int32_t K, int32_t rank) {
-  const int64_t blocks = (M + kDownRows - 1) / kDownRows * ((rank + 63) / 64);
-  const int64_t most = (K + kGroup * kDownNW - 1) / (kGroup * kDownNW);
-  const int64_t want = (256 + blocks - 1) / blocks;
-  return static_cast<int>(want < most ? want : most);
-}
-
 size_t u_bytes(int64_t M, int32_t K, int32_t rank) {
-  return static_cast<size_t>(down_slices(M, K, rank)) * M * rank * sizeof(float);
+  return static_cast<size_t>(lora_down_slices(M, K, rank)) * M * rank * sizeof(float);
 }
 
 }  // namespace
@@ -446,20 +437,9 @@ hipError_t launch_lora_tile(const LoraArgs& a, hipStream_t s) {
   g.w_bytes = static_cast<uint32_t>(static_cast<int64_t>(a.N) * g.Kw * 4);
   g.tmask = tail_mask(a.K);
   g.chunks = (g.Kw + 7) / 8;
-  // A wave per row and rank component while all of them are few rounds of the
-  // chip (both steps, rows and then k tiles, in us: 32 rows x 4096, rank 16, 28
-  // adapters 14.2 and 38.1; 777 x 1100, rank 8 17.1 and 24.8; 512 x 4096, rank
-  // 16 23.5 and 26.3; 1024 x 4096, rank 16 27.4 and 24.6; 4096 x 1024, rank 8
-  // 28.2 and 20.7).
-  const bool few_rows = static_cast<int64_t>(a.M) * (a.rank + 1) <= 16384;
-  g.slices = few_rows ? 1 : down_slices(a.M, a.K, a.rank);
-  // K split over a workgroup per 32 x 32 tile while they are about three per
-  // compute unit (128 rows, 4096 -> 4096, many adapters 18.7 us, in the larger
-  // tiles 33.6; one per 16 rows, rank 64 21.8 and 25.5; 256 rows 27.1 and 26.6).
-  const bool few_tiles = (a.M + 31) / 32 * words_of(a.N) <= 800;
-  const TileShape shape = tile_shape(a.N, g.chunks, 7000, 2500, [&](int rows) {
-    return static_cast<double>((a.M + rows - 1) / rows);
-  });
+  const bool by_rows = lora_down_by_rows(a.M, a.rank);
+  g.slices = lora_down_slices(a.M, a.K, a.rank);
+  const TileShape shape = lora_shape(a.M, a.N, g.chunks);
   g.wfl = shape.wfl;
   g.cols = static_cast<uint32_t>((a.N + shape.outputs() - 1) / shape.outputs());
   g.row_tiles = (a.M + shape.rows() - 1) / shape.rows();
@@ -470,7 +450,7 @@ hipError_t launch_lora_tile(const LoraArgs& a, hipStream_t s) {
     using T = decltype(v);
     const unsigned bx = static_cast<unsigned>((a.M + kDownRows - 1) / kDownRows);
     const unsigned by = static_cast<unsigned>(g.slices);
-    if (few_rows)
+    if (by_rows)
       launch_lora_down_rows(a, u, bits, s);
     else if (a.rank <= 16)
       lora_down_kernel<T, 1><<<dim3(bx, by, 1), kDownNT, 0, s>>>(a, u, bits, g.slices);
@@ -479,7 +459,7 @@ hipError_t launch_lora_tile(const LoraArgs& a, hipStream_t s) {
     else
       lora_down_kernel<T, 4><<<dim3(bx, by, static_cast<unsigned>((a.rank + 63) / 64)), kDownNT, 0,
                                s>>>(a, u, bits, g.slices);
-    if (few_tiles) {
+    if (lora_up_skinny(a.M, a.N)) {
       launch_lora_up_skinny(a, u, bits, g.slices, s);
       return;
     }

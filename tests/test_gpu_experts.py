@@ -30,6 +30,13 @@ LARGE = [
     (1500, 2, 4, 1000, 700, 0.02), (2000, 2, 5, 4097, 60, 0.0), (900, 3, 30, 1023, 515, 0.05),
     (3000, 1, 2, 700, 300, 0.0), (700, 4, 50, 640, 1030, 0.0), (33000, 1, 9, 33, 257, 0.02),
     (5000, 8, 64, 64, 1001, 0.01), (1, 16, 900, 4095, 5000, 0.0),
+    (300, 1, 40, 1029, 1030, 0.0), (600, 1, 40, 300, 2050, 0.02), (2050, 1, 2, 40, 2050, 0.0),
+    (300, 1, 40, 300, 4100, 0.1), (2050, 1, 40, 40, 2050, 0.0), (1030, 1, 40, 40, 4100, 0.05),
+]
+# Bits in whole tiles of every shape.
+TILES = [
+    (300, 1, 40, 40, 1030, 0.0), (300, 1, 40, 300, 2050, 0.02), (2050, 1, 9, 40, 2050, 0.0),
+    (300, 1, 40, 40, 4100, 0.1), (600, 1, 40, 300, 4100, 0.0), (1030, 1, 40, 40, 4100, 0.05),
 ]
 
 
@@ -58,7 +65,7 @@ def _dev(*arrays):
 
 
 @pytest.mark.parametrize("per_pair", [False, True])
-@pytest.mark.parametrize("case", CASES + LARGE[:8], ids=str)
+@pytest.mark.parametrize("case", CASES + LARGE[:8] + TILES, ids=str)
 def test_experts_fc(case, per_pair):
     T, k, E, K, N, none = case
     g = np.random.default_rng(T + K + N)

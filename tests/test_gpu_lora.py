@@ -33,6 +33,10 @@ CASES = [
     (500, 1029, 700, 4, 40, "bf16", "bf16"), (300, 1500, 300, 9, 136, "fp16", "fp32"),
     (1030, 643, 1100, 2, 16, "fp32", "fp32"), (200, 1000, 130, 70, 256, "fp32", "bf16"),
     (5000, 256, 64, 500, 16, "bf16", "bf16"), (3000, 512, 2050, 1, 64, "bf16", "bf16"),
+    (777, 40, 1030, 3, 8, "fp16", "bf16"), (400, 40, 8200, 2, 8, "bf16", "fp32"),
+    (1500, 40, 4100, 20, 8, "bf16", "bf16"), (600, 300, 8200, 5, 16, "fp32", "fp16"),
+    (900, 40, 8200, 4, 8, "fp16", "fp16"), (1500, 40, 8200, 6, 8, "fp32", "bf16"),
+    (3000, 40, 4100, 300, 16, "bf16", "fp32"),
 ]
 
 
