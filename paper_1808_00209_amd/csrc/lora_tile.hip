@@ -309,11 +309,13 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
   // once, whatever the adapters add up).  While one such step multiplies, the
   // next one's values are loaded, the next rows' first step among them.  A
   // row's outputs leave through LDS (a region per wave) as one run.
-  constexpr int kStride = 68;  // LDS words per row of 64 outputs
-  float* ts = reinterpret_cast<float*>(act) + wave * (33 * kStride);
-  float* al = ts + 32 * kStride;  // alpha of the wave's 64 outputs
-  constexpr int kV = 16 / sizeof(Y);  // outputs per 16-byte store
-  constexpr int kLanes = 64 / kV;     // lanes per row
+  constexpr int kV = 16 / sizeof(Y);    // outputs per 16-byte store
+  constexpr int kLanes = 64 / kV;       // lanes per row
+  constexpr int kStride = 64 + kV;      // LDS outputs per row of 64
+  constexpr int kRegion = 33 * 68 * 4;  // LDS bytes per wave
+  static_assert(32 * kStride * sizeof(Y) + 64 * sizeof(float) <= kRegion, "rows and alphas");
+  Y* ts = reinterpret_cast<Y*>(reinterpret_cast<char*>(act) + wave * kRegion);
+  float* al = reinterpret_cast<float*>(ts + 32 * kStride);  // alpha of the wave's 64 outputs
   const bool wide = a.N % kV == 0;
   al[lane] = f0 + lane < a.N && a.alpha ? a.alpha[f0 + lane] : 1.0f;
   const int base = m00 + t.wpi * PT * 32 + c;
@@ -383,19 +385,20 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
         const int n = 32 * tf + 2 * e + 4 * h;
-        const float4 f = *reinterpret_cast<const float4*>(&al[n]);
-        *reinterpret_cast<float4*>(&ts[c * kStride + n]) =
-            float4{acc[tf][pt][e] * f.x + low[tf][e], acc[tf][pt][e + 1] * f.y + low[tf][e + 1],
-                   acc[tf][pt][e + 2] * f.z + low[tf][e + 2],
-                   acc[tf][pt][e + 3] * f.w + low[tf][e + 3]};
+        float f[4];
+        __builtin_memcpy(f, __builtin_assume_aligned(&al[n], 16), sizeof(f));
+        Y y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          y[i] = from_f32<Y>(fmaf(acc[tf][pt][e + i], f[i], low[tf][e + i]));
+        __builtin_memcpy(__builtin_assume_aligned(&ts[c * kStride + n], sizeof(y)), y, sizeof(y));
       }
 #pragma unroll
     for (int o = 0; o < 32; o += 64 / kLanes) {
       const int i = o + lane / kLanes, col = kV * (lane % kLanes), n = f0 + col;
       const int m = __shfl(row[pt], i);
       Y v[kV];
-#pragma unroll
-      for (int e = 0; e < kV; ++e) v[e] = from_f32<Y>(ts[i * kStride + col + e]);
+      __builtin_memcpy(v, __builtin_assume_aligned(&ts[i * kStride + col], 16), sizeof(v));
       if (base - c + 32 * pt + i < a.M) {
         Y* dst = static_cast<Y*>(a.y) + static_cast<size_t>(m) * a.N + n;
         if (wide) {
