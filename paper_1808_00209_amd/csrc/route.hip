@@ -5,14 +5,16 @@
 // in each.  A key and its expert's index become one 64-bit number whose order
 // is that of the keys, equal keys lowest index first: the mantissa of a double
 // in [1, 2) holds the key's 32 bits made monotone and, below them, the index
-// from the top, so that one v_max_f64 compares both.  Every lane keeps its
-// three largest; a round takes the largest of the row's heads (DPP steps
-// within 16 lanes), and its lane moves up.  A lane that gave three looks
-// through its experts again, which few rows need.  The weights are computed
-// again for the chosen experts alone.
+// from the top, so that one v_max_f64 compares both.  Every lane keeps its four
+// largest; a round takes the largest of the row's heads (DPP steps within 16
+// lanes; of equal ones the lowest lane's, whose experts come first), and its
+// lane moves up.  A lane that gave four looks through its experts again (with
+// three kept, 43 % of the rows below did, 40 % of the kernel's instructions).
+// The weights are computed again for the chosen experts alone.
 //
 // 65521 rows of 256 experts in 8 groups, sigmoid scores and a bias: 67 MB of
-// logits, 13 us at 5.1 TB/s; a wave per row with shuffles took 139 us.
+// logits, 14 us at 5.1 TB/s; 27.6 us, bound by the vector ALU (1030
+// instructions for four rows).  A wave per row with shuffles took 139 us.
 #include <float.h>
 
 #include <type_traits>
@@ -24,6 +26,7 @@ namespace bnn {
 namespace {
 
 constexpr int kNT = 256;
+constexpr int kKeep = 4;             // experts that a lane holds ready
 constexpr float kNone = -INFINITY;  // the key of an expert out of reach
 
 struct RouteArgs {
@@ -42,10 +45,9 @@ __device__ __forceinline__ float dpp(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(v, v, CTRL, 0xF, 0xF, false));
 }
 template <int CTRL>
-__device__ __forceinline__ double dpp(double x) {
-  const int lo = __double2loint(x), hi = __double2hiint(x);
-  return __hiloint2double(__builtin_amdgcn_update_dpp(hi, hi, CTRL, 0xF, 0xF, false),
-                          __builtin_amdgcn_update_dpp(lo, lo, CTRL, 0xF, 0xF, false));
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  const int v = static_cast<int>(x);
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(v, v, CTRL, 0xF, 0xF, false));
 }
 
 // f over the LP lanes of a row; every lane gets the result.  f commutes, so
@@ -61,46 +63,51 @@ __device__ __forceinline__ V row_reduce(V x, F f) {
   return x;
 }
 
-// exp(z) within a few units of the last place: exp2 of the rounded z log2(e)
-// times 1 + the rest; 0 and infinity outside the normal range.
+// exp(z) within a few units of the last place for z in [-1000, 1000]: exp2 of
+// the rounded z log2(e) times 1 + the rest; 0 and infinity outside the normal
+// range.
 __device__ __forceinline__ float exp_of(float z) {
   constexpr float kL = 1.44269502162933349609375f;      // log2(e) rounded
   constexpr float kLlo = 1.925963033500011079e-8f;      // log2(e) - kL
   constexpr float kLn2 = 0.693147180559945309417f;
-  z = fminf(fmaxf(z, -1000.0f), 1000.0f);
   const float t = z * kL;
   const float rest = fmaf(z, kLlo, fmaf(z, kL, -t));
   return __builtin_amdgcn_exp2f(t) * fmaf(rest, kLn2, 1.0f);
 }
 
-// A logit as the score's argument; out of reach (-inf and NaN): kNone.
-__device__ __forceinline__ float argument(float raw, float scale) {
-  return raw > kNone ? fminf(fmaxf(raw * scale, -FLT_MAX), FLT_MAX) : kNone;
+// z within [-limit, limit].
+__device__ __forceinline__ float clamped(float z, float limit) {
+  return __builtin_amdgcn_fmed3f(z, -limit, limit);
 }
 
+// A logit in reach (not -inf or NaN) as its score; top and 1 / sum of the
+// row's softmax.  (A sigmoid's argument beyond +-1000 gives 0 or 1 as it is.)
 template <bool SOFTMAX>
-__device__ __forceinline__ float score(float z, float top, float inv_sum) {
-  if constexpr (SOFTMAX) return exp_of(z - top) * inv_sum;
-  return __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
+__device__ __forceinline__ float score(float raw, float scale, float top, float inv_sum) {
+  if constexpr (SOFTMAX)
+    return exp_of(clamped(clamped(raw * scale, FLT_MAX) - top, 1000.0f)) * inv_sum;
+  return __builtin_amdgcn_rcpf(1.0f + exp_of(clamped(-(raw * scale), 1000.0f)));
 }
 
-// Key and index as a double in [1, 2); kNone as the key of the index is the
-// smallest of all keys.
-__device__ __forceinline__ double pack_key(float key, int e) {
-  const uint32_t b = __float_as_uint(key);
-  const uint32_t u = b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+// A key made monotone and an index as a double in [1, 2); kNone is the smallest
+// of all keys.
+__device__ __forceinline__ double pack_bits_of(uint32_t u, int e) {
   return __hiloint2double(static_cast<int>(__builtin_amdgcn_alignbit(0x3FFu, u, 12)),
                           static_cast<int>((u << 20) | (0xFFFFFu - static_cast<uint32_t>(e))));
+}
+__device__ __forceinline__ double pack_key(float key, int e) {
+  const uint32_t b = __float_as_uint(key);
+  return pack_bits_of(b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u), e);
+}
+// Its parts: the key made monotone, and the index.
+__device__ __forceinline__ uint32_t key_of(double c) {
+  return __builtin_amdgcn_alignbit(static_cast<uint32_t>(__double2hiint(c)),
+                                   static_cast<uint32_t>(__double2loint(c)), 20);
 }
 __device__ __forceinline__ int index_of(double c) {
   return static_cast<int>(0xFFFFFu - (static_cast<uint32_t>(__double2loint(c)) & 0xFFFFFu));
 }
 constexpr uint32_t kNoneBits = 0x007FFFFFu;  // kNone made monotone
-__device__ __forceinline__ bool reachable(double c) {
-  const uint32_t u = __builtin_amdgcn_alignbit(static_cast<uint32_t>(__double2hiint(c)),
-                                               static_cast<uint32_t>(__double2loint(c)), 20);
-  return u > kNoneBits;
-}
 
 // (The library's fmax and fmin quiet signalling NaNs first, an instruction for
 // each operand; there are none here.)
@@ -128,26 +135,29 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
   const int e0 = ln * VPL;
 
   T raw[VPL];
-  float key[VPL];
+  float key[VPL];  // first the logits
   if (e0 + VPL <= a.E) {
     __builtin_memcpy(raw, src + e0, sizeof(raw));
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) key[i] = argument(to_f32(raw[i]), a.logit_scale);
+    for (int i = 0; i < VPL; ++i) key[i] = to_f32(raw[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      key[i] = e0 + i < a.E ? argument(to_f32(src[e0 + i]), a.logit_scale) : kNone;
+    for (int i = 0; i < VPL; ++i) key[i] = e0 + i < a.E ? to_f32(src[e0 + i]) : kNone;
   }
   float top = 0.0f, inv_sum = 1.0f;
   if constexpr (SOFTMAX) {
     top = kNone;
+    float ex[VPL];
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) top = fmaxf(top, key[i]);
+    for (int i = 0; i < VPL; ++i) {  // (false for NaN: out of reach as well)
+      ex[i] = key[i] > kNone ? clamped(key[i] * a.logit_scale, FLT_MAX) : kNone;
+      top = fmaxf(top, ex[i]);
+    }
     top = row_reduce<LP>(top, [](float x, float y) { return fmaxf(x, y); });
-    float sum = 0.0f, ex[VPL];
+    float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      ex[i] = key[i] > kNone ? exp_of(key[i] - top) : 0.0f;
+    for (int i = 0; i < VPL; ++i) {  // (0 where out of reach)
+      ex[i] = exp_of(clamped(ex[i] - top, 1000.0f));
       sum += ex[i];
     }
     sum = row_reduce<LP>(sum, [](float x, float y) { return x + y; });
@@ -158,7 +168,7 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
   } else {
 #pragma unroll
     for (int i = 0; i < VPL; ++i)
-      key[i] = key[i] > kNone ? score<false>(key[i], 0.0f, 0.0f) : kNone;
+      key[i] = key[i] > kNone ? score<false>(key[i], a.logit_scale, 0.0f, 0.0f) : kNone;
   }
   if (a.bias) {
     float b[VPL];
@@ -168,11 +178,9 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
 #pragma unroll
       for (int i = 0; i < VPL; ++i) b[i] = e0 + i < a.E ? a.bias[e0 + i] : 0.0f;
     }
+    // (the larger of NaN and kNone is kNone)
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      const float v = key[i] + b[i];
-      key[i] = v > kNone ? v : kNone;
-    }
+    for (int i = 0; i < VPL; ++i) key[i] = fmaxf(key[i] + b[i], kNone);
   }
 
   if (a.groups > 1) {
@@ -187,7 +195,7 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
       float2 b = {kNone, kNone};
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
-        b.y = fmaxf(b.y, fminf(b.x, key[i]));
+        b.y = __builtin_amdgcn_fmed3f(key[i], b.x, b.y);
         b.x = fmaxf(b.x, key[i]);
       }
       pairs[ln] = b;
@@ -245,47 +253,80 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
     }
   }
 
-  // The lane's three largest; those below `under` where it looks again.
-  double c0, c1, c2;
+  // The lane's largest (key, index); those below `under` where it looks again.
+  uint32_t u[kKeep];
+  int at[kKeep];
   auto largest = [&](auto again, double under) {
-    c0 = c1 = c2 = 0.0;
+    double best[kKeep] = {};
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
       double v = pack_key(key[i], e0 + i);
       if constexpr (decltype(again)::value) v = v < under ? v : 0.0;
-      const double v1 = min_f64(v, c0), v2 = min_f64(v1, c1);
-      c0 = max_f64(c0, v);
-      c1 = max_f64(c1, v1);
-      c2 = max_f64(c2, v2);
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q) {
+        const double less = min_f64(v, best[q]);
+        best[q] = max_f64(best[q], v);
+        v = less;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kKeep; ++q) {
+      u[q] = key_of(best[q]);
+      at[q] = index_of(best[q]);
     }
   };
   largest(std::false_type{}, 2.0);
-  int given = 0, my_id = -1;
-  double last = 2.0;
+  // A round takes the largest head of the row; of equal ones the lowest lane's,
+  // whose experts come first.  Its lane notes the expert and moves up.
+  __shared__ int32_t chosen[kRows][BNN_MAX_TOP_K];
+  const uint64_t my_row =
+      LP == 64 ? ~uint64_t{0}
+               : ((uint64_t{1} << (LP & 63)) - 1) << ((threadIdx.x & 63) / LP * LP);
+  int given = 0, last_i = 0;
+  uint32_t last_u = 0;
   for (int j = 0; j < a.k; ++j) {
-    if (VPL > 3 && __ballot(given == 3)) {
-      const double k0 = c0, k1 = c1, k2 = c2;
-      largest(std::true_type{}, last);
-      if (given != 3) {
-        c0 = k0;
-        c1 = k1;
-        c2 = k2;
+    if (VPL > kKeep && __ballot(given == kKeep)) {
+      uint32_t ku[kKeep];
+      int ka[kKeep];
+#pragma unroll
+      for (int q = 0; q < kKeep; ++q) {
+        ku[q] = u[q];
+        ka[q] = at[q];
+      }
+      largest(std::true_type{}, pack_bits_of(last_u, last_i));
+      if (given != kKeep) {
+#pragma unroll
+        for (int q = 0; q < kKeep; ++q) {
+          u[q] = ku[q];
+          at[q] = ka[q];
+        }
       } else {
         given = 0;
       }
     }
-    const double best = row_reduce<LP>(c0, max_f64);
-    if (ln == j && reachable(best)) my_id = index_of(best);
-    if (c0 == best) {  // (one lane of the row, or none has any left)
-      last = c0;
-      c0 = c1;
-      c1 = c2;
-      c2 = 0.0;
+    const uint32_t best =
+        row_reduce<LP>(u[0], [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    const uint64_t heads = __ballot(u[0] == best) & my_row;
+    if (u[0] == best && __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(heads >> 32),
+                                                  __builtin_amdgcn_mbcnt_lo(
+                                                      static_cast<uint32_t>(heads), 0)) == 0) {
+      chosen[row][j] = best > kNoneBits ? at[0] : -1;
+      last_u = u[0];
+      last_i = at[0];
+#pragma unroll
+      for (int q = 0; q + 1 < kKeep; ++q) {
+        u[q] = u[q + 1];
+        at[q] = at[q + 1];
+      }
+      u[kKeep - 1] = 0;
       ++given;
     }
   }
-  float w = my_id >= 0 ? score<SOFTMAX>(argument(to_f32(src[my_id]), a.logit_scale), top, inv_sum)
-                       : 0.0f;
+  // (a row's lanes are of one wave, whose LDS operations keep their order)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int my_id = ln < a.k ? chosen[row][ln] : -1;
+  float w = my_id >= 0 ? score<SOFTMAX>(to_f32(src[my_id]), a.logit_scale, top, inv_sum) : 0.0f;
   if (a.renorm) {
     const float total = row_reduce<LP>(w, [](float x, float y) { return x + y; });
     w = total > 0.0f ? w / total : 0.0f;
