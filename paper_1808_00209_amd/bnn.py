@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 
 import torch
@@ -581,6 +582,8 @@ def _rows(t, name):
     return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
 
 
+# (The sizes of workspaces are functions of the call's sizes alone: asked for
+# once for each, 0.6 us a call.)
 def _workspace(ws, need, like):
     """The caller's workspace, or a new one of `need` bytes beside like, and its
     size."""
@@ -621,6 +624,9 @@ def bnn_group_rows_workspace_size(M, G) -> int:
     return out.value
 
 
+_group_rows_bytes = functools.lru_cache(maxsize=1024)(bnn_group_rows_workspace_size)
+
+
 def bnn_group_rows(ids, G, offsets=None, order=None, workspace=None, stream=None):
     """Rows in the order of their group: ids (any shape, int32) -> (offsets
     [G + 1], order [ids.numel()]) int32; rows whose id is not in [0, G) come
@@ -630,7 +636,7 @@ def bnn_group_rows(ids, G, offsets=None, order=None, workspace=None, stream=None
     M = ids.numel()
     offsets = _output(offsets, ids, (G + 1,), torch.int32, "offsets")
     order = _output(order, ids, (M,), torch.int32, "order")
-    workspace, n = _workspace(workspace, bnn_group_rows_workspace_size(M, G), ids)
+    workspace, n = _workspace(workspace, _group_rows_bytes(M, G), ids)
     _check(lib.bnn_group_rows(M, G, _ptr(ids), _ptr(offsets), _ptr(order), _ptr(workspace), n,
                               _stream(stream)))
     return offsets, order
@@ -674,6 +680,11 @@ def bnn_experts_sum_workspace_size(desc: ExpertsDesc) -> int:
     return out.value
 
 
+@functools.lru_cache(maxsize=1024)
+def _experts_sum_bytes(*sizes):
+    return bnn_experts_sum_workspace_size(ExpertsDesc(*sizes))
+
+
 def bnn_experts_sum(x, K, w, ids, weights, offsets, order, alpha=None, dtype=torch.float32,
                     out=None, workspace=None, stream=None):
     """Binary FC layers of experts, weighted and added up per row: ids and
@@ -689,7 +700,8 @@ def bnn_experts_sum(x, K, w, ids, weights, offsets, order, alpha=None, dtype=tor
     dtype = dtype if out is None else out.dtype
     code = _real(dtype, "out")
     out = _output(out, x, (T, d.N), dtype, "out")
-    workspace, n = _workspace(workspace, bnn_experts_sum_workspace_size(d), x)
+    workspace, n = _workspace(
+        workspace, _experts_sum_bytes(T, top_k, d.E, d.N, d.K, d.share), x)
     _check(lib.bnn_experts_sum(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(ids), _ptr(weights),
                                _ptr(offsets), _ptr(order), _ptr(alpha), code, _ptr(out),
                                _ptr(workspace), n, _stream(stream)))
@@ -700,6 +712,11 @@ def bnn_bgemm_lora_workspace_size(desc: LoraDesc) -> int:
     out = ctypes.c_size_t()
     _check(load().bnn_bgemm_lora_workspace_size(ctypes.byref(desc), ctypes.byref(out)))
     return out.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _lora_bytes(*sizes):
+    return bnn_bgemm_lora_workspace_size(LoraDesc(*sizes))
 
 
 def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=None, dtype=None,
@@ -731,7 +748,7 @@ def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=N
     out_code = _real(dtype, "out")
     out = _output(out, x, (M, N), dtype, "out")
     d = LoraDesc(M, N, K, L, rank, code, out_code)
-    workspace, n = _workspace(workspace, bnn_bgemm_lora_workspace_size(d), x)
+    workspace, n = _workspace(workspace, _lora_bytes(M, N, K, L, rank, code, out_code), x)
     _check(lib.bnn_bgemm_lora(ctypes.byref(d), _ptr(x), stride, _ptr(offset), _ptr(w),
                               _ptr(alpha), _ptr(ids), _ptr(a), _ptr(b), _ptr(scale), _ptr(order),
                               _ptr(out), _ptr(workspace), n, _stream(stream)))
