@@ -3,10 +3,11 @@
 // an expert and 64, 128 or 256 outputs, the rows gathered through the order.
 //
 // 65536 pairs of 64 experts, 1024 -> 4096 to bits: 129 us, 4.2e15 operations a
-// second; 4096 -> 1024 to counts 115-125 us (the FC kernel without experts
+// second; 4096 -> 1024 to counts 113-122 us (the FC kernel without experts
 // reaches 5.5e15 at the clock that load allows).  The difference is row tiles
 // that experts do not fill and each block's start and end, at 1024 bits as long
-// as its four chunks.  One launch bound for all: the grid holds the most tiles
+// as its four chunks: there the matrix cores are busy in 47 % of the cycles, and
+// 6.3 vector instructions issue per MFMA.  One launch bound for all: the grid holds the most tiles
 // that there can be, blocks past the last one end at once.
 #include "expert_plans.hpp"
 #include "experts.hpp"
@@ -87,11 +88,15 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
     fl = __builtin_amdgcn_raw_buffer_load_b32(rflip, wi * 4, 0, 0);
   }
 
+  // Bits: S + 0.5 - thr, thresholds clamped to [-K-1, K+1], which keeps the
+  // comparison (|S| <= K).  Counts: S + K.
   v16f acc[2][PT];
 #pragma unroll
-  for (int tf = 0; tf < 2; ++tf)
-#pragma unroll
-    for (int pt = 0; pt < PT; ++pt) acc[tf][pt] = v16f{};
+  for (int tf = 0; tf < 2; ++tf) {
+    const float from = COUNTS ? static_cast<float>(a.K)
+                              : 0.5f - static_cast<float>(min(max(thv[tf], -a.K - 1), a.K + 1));
+    tile_start<PT>(acc[tf], h == 0 ? from : 0.0f);
+  }
   tile_loop<PT>(acc, act, t, [&] {
     return (static_cast<uint32_t>(pair_at(tid >> 1) / a.share) * a.Kw + 4 * (tid & 1)) * 4;
   });
@@ -103,7 +108,6 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
     // 32 rows x 64 outputs at a time through LDS (a region per wave), so that
     // a row's 64 counts are stored as one run of 128 bytes.
     uint16_t* ts = reinterpret_cast<uint16_t*>(act) + wave * (32 * kCountStride);
-    const float half = 0.5f * static_cast<float>(a.K);
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt) {
 #pragma unroll
@@ -113,7 +117,7 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
           uint32_t v[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            v[r] = static_cast<uint32_t>(0.5f * acc[tf][pt][4 * g + r] + half);
+            v[r] = static_cast<uint32_t>(0.5f * acc[tf][pt][4 * g + r]);
           *reinterpret_cast<uint2*>(&ts[c * kCountStride + 32 * tf + 8 * g + 4 * h]) =
               uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
         }
@@ -131,12 +135,6 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
       }
     }
   } else {
-    // Thresholds clamped to [-K-1, K+1], which keeps the comparison (|S| <= K).
-#pragma unroll
-    for (int tf = 0; tf < 2; ++tf)
-      tile_add<PT>(acc[tf], h == 0 ? 0.5f - static_cast<float>(
-                                                min(max(thv[tf], -a.K - 1), a.K + 1))
-                                   : 0.0f);
     const uint32_t fm = wi == a.Nw - 1 ? tail_mask(a.N) : ~0u;
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt) {

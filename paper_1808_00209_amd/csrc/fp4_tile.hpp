@@ -187,11 +187,12 @@ __device__ __forceinline__ void tile_loop(v16f (&acc)[2][PT], v4i* act, const Ti
   for (; ch < nch; ch += kRing) trip(ch, std::true_type{});
 }
 
-// Adds v to all 32 rows' sums of an output (lane c of half 0 holds output c's
-// value, the other half 0): one bf16 MFMA per tile, A an output's value as
-// three bf16 parts (exact: half-integers below 2^23), B ones.
+// Starts the sums of an output at v in all 32 rows (lane c of half 0 holds output
+// c's value, the other half 0): one bf16 MFMA per tile, where clearing its
+// registers takes 16 instructions; A an output's value as three bf16 parts
+// (exact: half-integers below 2^23), B ones.
 template <int PT>
-__device__ __forceinline__ void tile_add(v16f (&acc)[PT], float v) {
+__device__ __forceinline__ void tile_start(v16f (&acc)[PT], float v) {
   const uint16_t ones[8] = {kBf16One, kBf16One, kBf16One, kBf16One,
                             kBf16One, kBf16One, kBf16One, kBf16One};
   v4i b = __builtin_bit_cast(v4i, bf16x8(ones));
@@ -202,7 +203,7 @@ __device__ __forceinline__ void tile_add(v16f (&acc)[PT], float v) {
   for (int pt = 0; pt < PT; ++pt) {
     asm volatile("" : "+v"(b));  // (else one product and 16 PT moves)
     acc[pt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16x8(parts), __builtin_bit_cast(v8bf, b),
-                                                      acc[pt], 0, 0, 0);
+                                                      v16f{}, 0, 0, 0);
   }
 }
 
