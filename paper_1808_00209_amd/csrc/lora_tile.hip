@@ -5,11 +5,13 @@
 // and u lie by position.  A row's sums are taken in an order that does not
 // hang on the rows beside it.
 //
-// 8192 rows, 4096 -> 4096, 32 adapters of rank 16, bf16: x pass 32 us for 67 MB
-// (20 for x and its signs alone; the offsets, read through L1 as often as x,
-// add 5 and a 6), products and epilogue 70-74 (53 for the products to bits in
-// the FC kernel; the epilogue 14, all blocks in step, 8 of stores, 8 of
-// adapters).
+// 8192 rows, 4096 -> 4096, 32 adapters of rank 16, bf16: x pass 30 us for 67 MB
+// (20 for x and its signs alone, a 6; 32 where every lane loads the 8 offsets
+// it adds, as many bytes through L1 as x), products and epilogue 70 (53 for the
+// products to bits in the FC kernel; the epilogue 14, all blocks in step, 8 of
+// stores, 8 of adapters).
+#include <type_traits>
+
 #include "dtypes.hpp"
 #include "expert_plans.hpp"
 #include "experts.hpp"
@@ -61,6 +63,37 @@ __device__ __forceinline__ Frag<T> masked(const Frag<T>& f, uint32_t mask) {
   Frag<T> r;
   __builtin_memcpy(r.v, w, sizeof(w));
   return r;
+}
+
+// Lane 16 q + I's v in every lane of its row of 16 (DPP row_newbcast, taken by
+// the instruction that uses it).
+template <int I>
+__device__ __forceinline__ float of_row_lane(float v) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x150 + I, 0xF, 0xF, true));
+}
+
+// The signs of 8 sums x + off as a byte, element 0 in bit 7.  off's values are
+// those of lanes 8 P .. 8 P + 7 of the row.  A finite sum is above 0 where its
+// pattern is, as a whole number (it is not -0: off has none); then 0 - pattern
+// has the sign bit.
+template <int P, class T>
+__device__ __forceinline__ uint32_t sign_byte(const Frag<T>& x, float off) {
+  uint32_t byte = 0;
+  auto add = [&](auto e) {
+    constexpr int kE = decltype(e)::value;
+    byte = __builtin_amdgcn_alignbit(
+        byte, 0u - __float_as_uint(to_f32(x.v[kE]) + of_row_lane<8 * P + kE>(off)), 31);
+  };
+  add(std::integral_constant<int, 0>{});
+  add(std::integral_constant<int, 1>{});
+  add(std::integral_constant<int, 2>{});
+  add(std::integral_constant<int, 3>{});
+  add(std::integral_constant<int, 4>{});
+  add(std::integral_constant<int, 5>{});
+  add(std::integral_constant<int, 6>{});
+  add(std::integral_constant<int, 7>{});
+  return byte;
 }
 
 __device__ __forceinline__ v4f mma16(const Frag<__bf16>& x, const Frag<__bf16>& y, v4f acc) {
@@ -167,26 +200,27 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
       }
     }
   };
-  auto make_bits = [&](const Xs& x, int g, auto full) {
+  // The offsets of a group, an element per lane and load: lane (q, c) has
+  // element c % 8 of its q's eight, of the 32 k of step 2 j + c / 8.
+  float off[2] = {0.0f, 0.0f};
+  auto load_off = [&](int g, auto full) {
+    if (!want_bits || !a.offset) return;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int k = g * kGroup + 32 * (2 * j + (c >> 3)) + 8 * q + (c & 7);
+      off[j] = decltype(full)::value || k < a.K ? a.offset[k] : 0.0f;
+    }
+  };
+  // Elements past K are 0 with offset 0: bit 0.
+  auto make_bits = [&](const Xs& x, int g) {
     uint32_t w[kDownRW][4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int k = g * kGroup + 32 * s + 8 * q;
-      Frag<float> off = {};
-      if (a.offset) off = load_frag<decltype(full)::value, float>(a.offset + k, a.K - k);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) off.v[e] += 0.0f;  // -0 to +0
+    for (int j = 0; j < 2; ++j) {
+      const float o = off[j] + 0.0f;  // -0 to +0
 #pragma unroll
       for (int i = 0; i < kDownRW; ++i) {
-        // A finite sum is above 0 where its pattern is, as a whole number (it
-        // is not -0: off has none); then 0 - pattern has the sign bit.
-        // Elements past K are 0 with offset 0: bit 0.
-        uint32_t byte = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          byte = __builtin_amdgcn_alignbit(
-              byte, 0u - __float_as_uint(to_f32(x[s][i].v[e]) + off.v[e]), 31);
-        w[i][s] = byte << (24 - 8 * q);
+        w[i][2 * j] = sign_byte<0>(x[2 * j][i], o) << (24 - 8 * q);
+        w[i][2 * j + 1] = sign_byte<1>(x[2 * j + 1][i], o) << (24 - 8 * q);
       }
     }
 #pragma unroll
@@ -215,6 +249,7 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
     if (kAhead && nd) load_a(w, 0, g, std::true_type{});
     for (; g < whole; ++g) {
       Xs next;
+      load_off(g, std::true_type{});
       load_x(next, min(g + 1, whole - 1), std::true_type{});
       for (int d = 0; d < nd; ++d) {
         if constexpr (kAhead) {
@@ -228,17 +263,18 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
           multiply(x, w, d);
         }
       }
-      if (want_bits) make_bits(x, g, std::true_type{});
+      if (want_bits) make_bits(x, g);
       __builtin_memcpy(&x, &next, sizeof(x));
     }
   }
   if (g < end) {
     load_x(x, g, std::false_type{});
+    load_off(g, std::false_type{});
     for (int d = 0; d < nd; ++d) {
       load_a(w, d, g, std::false_type{});
       multiply(x, w, d);
     }
-    if (want_bits) make_bits(x, g, std::false_type{});
+    if (want_bits) make_bits(x, g);
   }
   // The waves' parts of u meet in LDS, added in the waves' order.
 #pragma unroll
