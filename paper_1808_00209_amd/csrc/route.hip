@@ -2,19 +2,20 @@
 // largest keys and their weights (bnn_route).
 //
 // A row's E logits lie in the registers of LP lanes, VPL consecutive experts
-// in each.  A key and its expert's index become one 64-bit number whose order
-// is that of the keys, equal keys lowest index first: the mantissa of a double
-// in [1, 2) holds the key's 32 bits made monotone and, below them, the index
-// from the top, so that one v_max_f64 compares both.  Every lane keeps its four
-// largest; a round takes the largest of the row's heads (DPP steps within 16
-// lanes; of equal ones the lowest lane's, whose experts come first), and its
-// lane moves up.  A lane that gave four looks through its experts again (with
-// three kept, 43 % of the rows below did, 40 % of the kernel's instructions).
-// The weights are computed again for the chosen experts alone.
+// in each.  Every lane keeps its four largest keys, in order (v_med3_f32 puts a
+// key in its place, an instruction for each of the four).  A round takes the
+// largest of the row's heads, as whole numbers of the keys' order (DPP steps
+// within 16 lanes; of equal ones the lowest lane's, whose experts come first),
+// and its lane moves up, noting the key and how many equal ones it gave before.
+// A lane that gave four looks through its keys again.  Which expert of the lane
+// a key belongs to is found at the end, once for each of the top_k, from the
+// keys in LDS.  The weights are computed again for the chosen experts alone.
 //
 // 65521 rows of 256 experts in 8 groups, sigmoid scores and a bias: 67 MB of
-// logits, 14 us at 5.1 TB/s; 27.6 us, bound by the vector ALU (1030
-// instructions for four rows).  A wave per row with shuffles took 139 us.
+// logits, 14 us at 5.1 TB/s; 24.9 us, the vector ALU busy in three quarters of
+// them (854 instructions for four rows; with the experts' indices carried along
+// in the low bits of doubles 1030 and 27.7 us).  A wave per row with shuffles
+// took 139 us.
 #include <float.h>
 
 #include <type_traits>
@@ -80,6 +81,12 @@ __device__ __forceinline__ float clamped(float z, float limit) {
   return __builtin_amdgcn_fmed3f(z, -limit, limit);
 }
 
+// The larger of two numbers that are not NaN (fmaxf quiets signalling ones
+// first, an instruction for each operand).
+__device__ __forceinline__ float larger(float x, float y) {
+  return __builtin_amdgcn_fmed3f(x, y, INFINITY);
+}
+
 // A logit in reach (not -inf or NaN) as its score; top and 1 / sum of the
 // row's softmax.  (A sigmoid's argument beyond +-1000 gives 0 or 1 as it is.)
 template <bool SOFTMAX>
@@ -89,38 +96,15 @@ __device__ __forceinline__ float score(float raw, float scale, float top, float 
   return __builtin_amdgcn_rcpf(1.0f + exp_of(clamped(-(raw * scale), 1000.0f)));
 }
 
-// A key made monotone and an index as a double in [1, 2); kNone is the smallest
-// of all keys.
-__device__ __forceinline__ double pack_bits_of(uint32_t u, int e) {
-  return __hiloint2double(static_cast<int>(__builtin_amdgcn_alignbit(0x3FFu, u, 12)),
-                          static_cast<int>((u << 20) | (0xFFFFFu - static_cast<uint32_t>(e))));
-}
-__device__ __forceinline__ double pack_key(float key, int e) {
+// A key as a whole number of the same order, and back.
+__device__ __forceinline__ uint32_t ordered(float key) {
   const uint32_t b = __float_as_uint(key);
-  return pack_bits_of(b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u), e);
+  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
 }
-// Its parts: the key made monotone, and the index.
-__device__ __forceinline__ uint32_t key_of(double c) {
-  return __builtin_amdgcn_alignbit(static_cast<uint32_t>(__double2hiint(c)),
-                                   static_cast<uint32_t>(__double2loint(c)), 20);
+__device__ __forceinline__ float unordered(uint32_t u) {
+  return __uint_as_float(u ^ (static_cast<uint32_t>(~static_cast<int32_t>(u) >> 31) | 0x80000000u));
 }
-__device__ __forceinline__ int index_of(double c) {
-  return static_cast<int>(0xFFFFFu - (static_cast<uint32_t>(__double2loint(c)) & 0xFFFFFu));
-}
-constexpr uint32_t kNoneBits = 0x007FFFFFu;  // kNone made monotone
-
-// (The library's fmax and fmin quiet signalling NaNs first, an instruction for
-// each operand; there are none here.)
-__device__ __forceinline__ double max_f64(double x, double y) {
-  double d;
-  asm("v_max_f64 %0, %1, %2" : "=v"(d) : "v"(x), "v"(y));
-  return d;
-}
-__device__ __forceinline__ double min_f64(double x, double y) {
-  double d;
-  asm("v_min_f64 %0, %1, %2" : "=v"(d) : "v"(x), "v"(y));
-  return d;
-}
+constexpr uint32_t kNoneBits = 0x007FFFFFu;  // ordered(kNone)
 
 // LP lanes per row, VPL experts per lane.
 template <int LP, int VPL, bool SOFTMAX, class T>
@@ -167,8 +151,10 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
     for (int i = 0; i < VPL; ++i) key[i] = key[i] > kNone ? ex[i] * inv_sum : kNone;
   } else {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      key[i] = key[i] > kNone ? score<false>(key[i], a.logit_scale, 0.0f, 0.0f) : kNone;
+    for (int i = 0; i < VPL; ++i) {
+      const float v = score<false>(key[i], a.logit_scale, 0.0f, 0.0f);
+      key[i] = key[i] > kNone ? v : kNone;
+    }
   }
   if (a.bias) {
     float b[VPL];
@@ -196,7 +182,7 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
         b.y = __builtin_amdgcn_fmed3f(key[i], b.x, b.y);
-        b.x = fmaxf(b.x, key[i]);
+        b.x = larger(b.x, key[i]);
       }
       pairs[ln] = b;
     } else {
@@ -211,14 +197,14 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
         const int n = a.per_group / VPL;
         for (int j = 0; j < n; ++j) {
           const float2 v = pairs[g * n + j];
-          b1 = fmaxf(fmaxf(b1, v.y), fminf(b0, v.x));
-          b0 = fmaxf(b0, v.x);
+          b1 = larger(__builtin_amdgcn_fmed3f(b0, b1, v.x), v.y);
+          b0 = larger(b0, v.x);
         }
       } else {
         for (int j = 0; j < a.per_group; ++j) {
           const float v = keys[g * a.per_group + j];
-          b1 = fmaxf(b1, fminf(b0, v));
-          b0 = fmaxf(b0, v);
+          b1 = __builtin_amdgcn_fmed3f(b0, b1, v);
+          b0 = larger(b0, v);
         }
       }
       scores[g] = a.group_top == 2 && b1 > kNone ? b0 + b1 : b0;
@@ -253,71 +239,71 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
     }
   }
 
-  // The lane's largest (key, index); those below `under` where it looks again.
+  // The lane's largest keys; where it looks again, without those above `last`
+  // and the first `skip` of those equal to it.
   uint32_t u[kKeep];
-  int at[kKeep];
-  auto largest = [&](auto again, double under) {
-    double best[kKeep] = {};
+  auto largest = [&](auto again, float last, int skip) {
+    float best[kKeep];
+#pragma unroll
+    for (int q = 0; q < kKeep; ++q) best[q] = kNone;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-      double v = pack_key(key[i], e0 + i);
-      if constexpr (decltype(again)::value) v = v < under ? v : 0.0;
-#pragma unroll
-      for (int q = 0; q < kKeep; ++q) {
-        const double less = min_f64(v, best[q]);
-        best[q] = max_f64(best[q], v);
-        v = less;
+      float v = key[i];
+      if constexpr (decltype(again)::value) {
+        const bool same = v == last;
+        v = v < last || (same && skip <= 0) ? v : kNone;
+        skip -= same ? 1 : 0;
       }
+#pragma unroll
+      for (int q = kKeep - 1; q > 0; --q)
+        best[q] = __builtin_amdgcn_fmed3f(v, best[q - 1], best[q]);
+      best[0] = larger(v, best[0]);
     }
 #pragma unroll
-    for (int q = 0; q < kKeep; ++q) {
-      u[q] = key_of(best[q]);
-      at[q] = index_of(best[q]);
-    }
+    for (int q = 0; q < kKeep; ++q) u[q] = ordered(best[q]);
   };
-  largest(std::false_type{}, 2.0);
+  largest(std::false_type{}, 0.0f, 0);
+  constexpr int kStride = VPL + 4;  // LDS floats per lane: 16-byte rows, spread over the banks
+  __shared__ __attribute__((aligned(16))) float all[kRows][LP * kStride];
+#pragma unroll
+  for (int i = 0; i < VPL; i += 4)
+    *reinterpret_cast<float4*>(&all[row][ln * kStride + i]) =
+        float4{key[i], key[i + 1], key[i + 2], key[i + 3]};
   // A round takes the largest head of the row; of equal ones the lowest lane's,
-  // whose experts come first.  Its lane notes the expert and moves up.
-  __shared__ int32_t chosen[kRows][BNN_MAX_TOP_K];
+  // whose experts come first.  Its lane notes itself, the key, and how many
+  // equal ones it gave before, and moves up.
+  __shared__ uint2 chosen[kRows][BNN_MAX_TOP_K];
   const uint64_t my_row =
       LP == 64 ? ~uint64_t{0}
                : ((uint64_t{1} << (LP & 63)) - 1) << ((threadIdx.x & 63) / LP * LP);
-  int given = 0, last_i = 0;
-  uint32_t last_u = 0;
+  int given = 0, same = 0;
+  uint32_t last = 0;
   for (int j = 0; j < a.k; ++j) {
     if (VPL > kKeep && __ballot(given == kKeep)) {
-      uint32_t ku[kKeep];
-      int ka[kKeep];
+      uint32_t held[kKeep];
 #pragma unroll
-      for (int q = 0; q < kKeep; ++q) {
-        ku[q] = u[q];
-        ka[q] = at[q];
-      }
-      largest(std::true_type{}, pack_bits_of(last_u, last_i));
-      if (given != kKeep) {
+      for (int q = 0; q < kKeep; ++q) held[q] = u[q];
+      largest(std::true_type{}, unordered(last), same + 1);
 #pragma unroll
-        for (int q = 0; q < kKeep; ++q) {
-          u[q] = ku[q];
-          at[q] = ka[q];
-        }
-      } else {
-        given = 0;
-      }
+      for (int q = 0; q < kKeep; ++q) u[q] = given == kKeep ? u[q] : held[q];
+      given = given == kKeep ? 0 : given;
     }
     const uint32_t best =
         row_reduce<LP>(u[0], [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-    const uint64_t heads = __ballot(u[0] == best) & my_row;
-    if (u[0] == best && __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(heads >> 32),
-                                                  __builtin_amdgcn_mbcnt_lo(
-                                                      static_cast<uint32_t>(heads), 0)) == 0) {
-      chosen[row][j] = best > kNoneBits ? at[0] : -1;
-      last_u = u[0];
-      last_i = at[0];
+    bool mine = u[0] == best;
+    uint64_t heads = __ballot(mine);
+    if (__popcll(heads) != 64 / LP) {  // (else one in every row)
+      heads &= my_row;
+      mine = mine && __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(heads >> 32),
+                                               __builtin_amdgcn_mbcnt_lo(
+                                                   static_cast<uint32_t>(heads), 0)) == 0;
+    }
+    if (mine) {
+      same = best == last ? same + 1 : 0;
+      last = best;
+      chosen[row][j] = uint2{best, static_cast<uint32_t>(ln | same << 8)};
 #pragma unroll
-      for (int q = 0; q + 1 < kKeep; ++q) {
-        u[q] = u[q + 1];
-        at[q] = at[q + 1];
-      }
+      for (int q = 0; q + 1 < kKeep; ++q) u[q] = u[q + 1];
       u[kKeep - 1] = 0;
       ++given;
     }
@@ -325,7 +311,31 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
   // (a row's lanes are of one wave, whose LDS operations keep their order)
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  const int my_id = ln < a.k ? chosen[row][ln] : -1;
+  // Lane j finds the j-th expert among those of the lane that gave it.
+  int my_id = -1;
+  if (ln < a.k) {
+    const uint2 note = chosen[row][ln];
+    const float mine = unordered(note.x);
+    const int from = static_cast<int>(note.y & 255u);
+    int before = static_cast<int>(note.y >> 8), at = 0;
+    float v[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; i += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(&all[row][from * kStride + i]);
+      v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
+    }
+    if (__ballot(before > 0)) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        at = v[i] == mine && before == 0 ? i : at;
+        before -= v[i] == mine ? 1 : 0;
+      }
+    } else {
+#pragma unroll
+      for (int i = VPL - 1; i >= 0; --i) at = v[i] == mine ? i : at;
+    }
+    if (note.x > kNoneBits) my_id = from * VPL + at;
+  }
   float w = my_id >= 0 ? score<SOFTMAX>(to_f32(src[my_id]), a.logit_scale, top, inv_sum) : 0.0f;
   if (a.renorm) {
     const float total = row_reduce<LP>(w, [](float x, float y) { return x + y; });
