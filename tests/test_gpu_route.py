@@ -77,6 +77,24 @@ def test_ties_go_to_the_lowest_index():
         _check(x, min(E, 9), score="sigmoid")
 
 
+@pytest.mark.parametrize("E", [16, 60, 128, 250, 256, 640, 1024])
+def test_few_distinct_keys(E):
+    # Runs of equal keys that begin and end anywhere, longer and shorter than
+    # what is held ready of one stretch of experts, closed ones between them.
+    g = np.random.default_rng(E)
+    x = g.integers(0, 3, size=(40, E)).astype(np.float32)
+    for t in range(0, 40, 2):
+        x[t] = 0.0
+        at = int(g.integers(0, E))
+        x[t, at:at + int(g.integers(1, 20))] = 1.0
+    x[g.random((40, E)) < 0.2] = -float("inf")
+    x = torch.from_numpy(x)
+    for k in (1, 5, min(E, 16)):
+        _check(x, k)
+        _check(x, k, score="sigmoid")
+        _check(x, k, score="sigmoid", groups=2, top_groups=1, group_top=2)
+
+
 @pytest.mark.parametrize("kind", ["fp32", "fp16", "bf16"])
 def test_the_lowest_value_is_no_mask_and_minus_infinity_is(kind):
     t = TYPES[kind]
