@@ -576,10 +576,16 @@ def _output(t, like, shape, dtype, name):
 
 
 def _rows(t, name):
-    """A 2-d tensor whose rows are contiguous: their distance in elements."""
+    """A 2-d tensor whose rows are contiguous and do not overlap: their distance
+    in elements."""
     if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("%s must be a 2-d CUDA(HIP) tensor with contiguous rows" % name)
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    if t.shape[0] < 2:
+        return t.shape[1]
+    if t.stride(0) < t.shape[1]:
+        raise ValueError("the rows of %s overlap (%d elements long, %d apart): call contiguous()"
+                         % (name, t.shape[1], t.stride(0)))
+    return t.stride(0)
 
 
 # (The sizes of workspaces are functions of the call's sizes alone: asked for
