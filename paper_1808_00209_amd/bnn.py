@@ -568,10 +568,30 @@ def _shaped(t, shape, name):
     return t
 
 
-def _output(t, like, shape, dtype, name):
+# A call's memory belongs to the stream that the call runs on (new_empty of a
+# tensor on the current one): torch's allocator may hand the block to other work
+# of that stream as soon as the tensor is dropped, and to no other's.
+def _scratch(like, shape, dtype, stream):
+    """A new tensor on like's device for the call alone."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _empty(like, shape, dtype, stream):
+    """A new tensor on like's device that the caller gets, and may use and drop
+    on the current stream."""
+    t = _scratch(like, shape, dtype, stream)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(like.device))
+    return t
+
+
+def _output(t, like, shape, dtype, name, stream):
     """A new tensor on like's device, or the caller's, looked at."""
     if t is None:
-        return like.new_empty(shape, dtype=dtype)
+        return _empty(like, shape, dtype, stream)
     return _shaped(_dev(t, dtype, name), shape, name)
 
 
@@ -590,11 +610,11 @@ def _rows(t, name):
 
 # (The sizes of workspaces are functions of the call's sizes alone: asked for
 # once for each, 0.6 us a call.)
-def _workspace(ws, need, like):
+def _workspace(ws, need, like, stream):
     """The caller's workspace, or a new one of `need` bytes beside like, and its
     size."""
     if ws is None:
-        return (like.new_empty(need, dtype=torch.uint8) if need else None), need
+        return (_scratch(like, need, torch.uint8, stream) if need else None), need
     return ws, _dev(ws, torch.uint8, "workspace").numel()
 
 
@@ -613,8 +633,8 @@ def bnn_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=No
     stride = _rows(logits, "logits")
     T, E = logits.shape
     bias = _shaped(_dev(bias, torch.float32, "bias"), (E,), "bias")
-    ids = _output(ids, logits, (T, top_k), torch.int32, "ids")
-    weights = _output(weights, logits, (T, top_k), torch.float32, "weights")
+    ids = _output(ids, logits, (T, top_k), torch.int32, "ids", stream)
+    weights = _output(weights, logits, (T, top_k), torch.float32, "weights", stream)
     if score not in _SCORES:
         raise ValueError("score must be one of %s" % sorted(_SCORES))
     d = RouteDesc(E, top_k, groups, groups if top_groups is None else top_groups, group_top,
@@ -640,9 +660,9 @@ def bnn_group_rows(ids, G, offsets=None, order=None, workspace=None, stream=None
     lib = load()
     _dev(ids, torch.int32, "ids")
     M = ids.numel()
-    offsets = _output(offsets, ids, (G + 1,), torch.int32, "offsets")
-    order = _output(order, ids, (M,), torch.int32, "order")
-    workspace, n = _workspace(workspace, _group_rows_bytes(M, G), ids)
+    offsets = _output(offsets, ids, (G + 1,), torch.int32, "offsets", stream)
+    order = _output(order, ids, (M,), torch.int32, "order", stream)
+    workspace, n = _workspace(workspace, _group_rows_bytes(M, G), ids, stream)
     _check(lib.bnn_group_rows(M, G, _ptr(ids), _ptr(offsets), _ptr(order), _ptr(workspace), n,
                               _stream(stream)))
     return offsets, order
@@ -674,7 +694,7 @@ def bnn_experts_fc(x, K, w, offsets, order, thr, flip=None, out_bits=None, strea
     nw = words(d.N)
     _shaped(_dev(thr, torch.int32, "thr"), (d.E, d.N), "thr")
     _shaped(_dev(flip, torch.int32, "flip"), (d.E, nw), "flip")
-    out_bits = _output(out_bits, x, (M, nw), torch.int32, "out_bits")
+    out_bits = _output(out_bits, x, (M, nw), torch.int32, "out_bits", stream)
     _check(lib.bnn_experts_fc(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(offsets), _ptr(order),
                               _ptr(thr), _ptr(flip), _ptr(out_bits), _stream(stream)))
     return out_bits
@@ -705,9 +725,9 @@ def bnn_experts_sum(x, K, w, ids, weights, offsets, order, alpha=None, dtype=tor
     _shaped(_dev(alpha, torch.float32, "alpha"), (d.E, d.N), "alpha")
     dtype = dtype if out is None else out.dtype
     code = _real(dtype, "out")
-    out = _output(out, x, (T, d.N), dtype, "out")
+    out = _output(out, x, (T, d.N), dtype, "out", stream)
     workspace, n = _workspace(
-        workspace, _experts_sum_bytes(T, top_k, d.E, d.N, d.K, d.share), x)
+        workspace, _experts_sum_bytes(T, top_k, d.E, d.N, d.K, d.share), x, stream)
     _check(lib.bnn_experts_sum(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(ids), _ptr(weights),
                                _ptr(offsets), _ptr(order), _ptr(alpha), code, _ptr(out),
                                _ptr(workspace), n, _stream(stream)))
@@ -752,9 +772,10 @@ def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=N
     _shaped(_dev(offset, torch.float32, "offset"), (K,), "offset")
     dtype = out.dtype if out is not None else kind if dtype is None else dtype
     out_code = _real(dtype, "out")
-    out = _output(out, x, (M, N), dtype, "out")
+    out = _output(out, x, (M, N), dtype, "out", stream)
     d = LoraDesc(M, N, K, L, rank, code, out_code)
-    workspace, n = _workspace(workspace, _lora_bytes(M, N, K, L, rank, code, out_code), x)
+    workspace, n = _workspace(workspace, _lora_bytes(M, N, K, L, rank, code, out_code), x,
+                              stream)
     _check(lib.bnn_bgemm_lora(ctypes.byref(d), _ptr(x), stride, _ptr(offset), _ptr(w),
                               _ptr(alpha), _ptr(ids), _ptr(a), _ptr(b), _ptr(scale), _ptr(order),
                               _ptr(out), _ptr(workspace), n, _stream(stream)))
