@@ -201,6 +201,27 @@ def _dev(t, dtype, name):
     return t
 
 
+# A call's memory belongs to the stream that the call runs on (new_empty of a
+# tensor on the current one): torch's allocator may hand the block to other work
+# of that stream as soon as the tensor is dropped, and to no other's.
+def _scratch(like, shape, dtype, stream):
+    """A new tensor on like's device for the call alone."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _empty(like, shape, dtype, stream):
+    """A new tensor on like's device that the caller gets, and may use and drop
+    on the current stream."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    t = _scratch(like, shape, dtype, stream)
+    t.record_stream(torch.cuda.current_stream(like.device))
+    return t
+
+
 def words(bits: int) -> int:
     return (bits + 31) // 32
 
@@ -257,7 +278,7 @@ def bnn_pack_bits(x, offset=None, out=None, stream=None):
     if offset is not None:
         offset = _dev(offset, torch.float32, "offset")
     if out is None:
-        out = torch.empty(tuple(x.shape[:-1]) + (words(D),), dtype=torch.int32, device=x.device)
+        out = _empty(x, tuple(x.shape[:-1]) + (words(D),), torch.int32, stream)
     _u32(out)
     _check(lib.bnn_pack_bits(_ptr(x), _ptr(offset), rows, D, _ptr(out), _stream(stream)))
     return out
@@ -301,10 +322,9 @@ def bnn_bconv2d(desc: ConvDesc, x, w, thr=None, flip=None, want_sums=True, want_
     thr = _dev(thr, torch.int32, "thr")
     flip = _dev(flip, torch.int32, "flip")
     if want_sums and out_sums is None:
-        out_sums = torch.empty((desc.N, Ho, Wo, desc.F), dtype=torch.int32, device=x.device)
+        out_sums = _empty(x, (desc.N, Ho, Wo, desc.F), torch.int32, stream)
     if want_bits and out_bits is None:
-        out_bits = torch.empty((desc.N, Hp, Wp, words(desc.F)), dtype=torch.int32,
-                               device=x.device)
+        out_bits = _empty(x, (desc.N, Hp, Wp, words(desc.F)), torch.int32, stream)
     _check(lib.bnn_bconv2d(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(thr), _ptr(flip),
                            _ptr(out_sums), _ptr(out_bits), _stream(stream)))
     return out_sums, out_bits
@@ -322,8 +342,7 @@ def bnn_prepare_weights(w, F, KH, KW, C, out=None, stream=None):
     lib = load()
     _u32(w)
     if out is None:
-        out = torch.empty(bnn_prepared_weights_size(F, KH, KW, C), dtype=torch.uint8,
-                          device=w.device)
+        out = _empty(w, bnn_prepared_weights_size(F, KH, KW, C), torch.uint8, stream)
     _check(lib.bnn_prepare_weights(F, KH, KW, C, _ptr(w), _ptr(out), _stream(stream)))
     return out
 
@@ -339,10 +358,9 @@ def bnn_bconv2d_prepared(desc: ConvDesc, x, w, wprep, thr=None, flip=None, want_
     thr = _dev(thr, torch.int32, "thr")
     flip = _dev(flip, torch.int32, "flip")
     if want_sums and out_sums is None:
-        out_sums = torch.empty((desc.N, Ho, Wo, desc.F), dtype=torch.int32, device=x.device)
+        out_sums = _empty(x, (desc.N, Ho, Wo, desc.F), torch.int32, stream)
     if want_bits and out_bits is None:
-        out_bits = torch.empty((desc.N, Hp, Wp, words(desc.F)), dtype=torch.int32,
-                               device=x.device)
+        out_bits = _empty(x, (desc.N, Hp, Wp, words(desc.F)), torch.int32, stream)
     _check(lib.bnn_bconv2d_prepared(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(wprep), _ptr(thr),
                                     _ptr(flip), _ptr(out_sums), _ptr(out_bits),
                                     _stream(stream)))
@@ -359,10 +377,9 @@ def bnn_fconv2d_binw(desc: ConvDesc, x, w, thr=None, flip=None, want_sums=True,
     thr = _dev(thr, torch.int32, "thr")
     flip = _dev(flip, torch.int32, "flip")
     if want_sums and out_sums is None:
-        out_sums = torch.empty((desc.N, Ho, Wo, desc.F), dtype=torch.float32, device=x.device)
+        out_sums = _empty(x, (desc.N, Ho, Wo, desc.F), torch.float32, stream)
     if want_bits and out_bits is None:
-        out_bits = torch.empty((desc.N, Hp, Wp, words(desc.F)), dtype=torch.int32,
-                               device=x.device)
+        out_bits = _empty(x, (desc.N, Hp, Wp, words(desc.F)), torch.int32, stream)
     _check(lib.bnn_fconv2d_binw(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(thr), _ptr(flip),
                                 _ptr(out_sums), _ptr(out_bits), _stream(stream)))
     return out_sums, out_bits
@@ -376,7 +393,7 @@ def bnn_binarize_input(mode, x, offset=None, out=None, stream=None):
     offset = _dev(offset, torch.float32, "offset")
     N, H, W, Cin = x.shape
     if out is None:
-        out = torch.empty((N, H, W, 1), dtype=torch.int32, device=x.device)
+        out = _empty(x, (N, H, W, 1), torch.int32, stream)
     _check(lib.bnn_binarize_input(int(mode), _ptr(x), _ptr(offset), N, H, W, Cin, _ptr(out),
                                   _stream(stream)))
     return out
@@ -396,10 +413,9 @@ def bnn_bconv2d_input(desc: ConvDesc, mode, x, offset, w, thr=None, flip=None, w
     thr = _dev(thr, torch.int32, "thr")
     flip = _dev(flip, torch.int32, "flip")
     if want_sums and out_sums is None:
-        out_sums = torch.empty((desc.N, Ho, Wo, desc.F), dtype=torch.int32, device=x.device)
+        out_sums = _empty(x, (desc.N, Ho, Wo, desc.F), torch.int32, stream)
     if want_bits and out_bits is None:
-        out_bits = torch.empty((desc.N, Hp, Wp, words(desc.F)), dtype=torch.int32,
-                               device=x.device)
+        out_bits = _empty(x, (desc.N, Hp, Wp, words(desc.F)), torch.int32, stream)
     _check(lib.bnn_bconv2d_input(ctypes.byref(desc), int(mode), _ptr(x), _ptr(offset), _ptr(w),
                                  _ptr(thr), _ptr(flip), _ptr(out_sums), _ptr(out_bits),
                                  _stream(stream)))
@@ -422,8 +438,7 @@ def bnn_fconv_bconv2d(desc0: ConvDesc, desc1: ConvDesc, x, w0, thr0, flip0, w1, 
     flip0 = _dev(flip0, torch.int32, "flip0")
     flip1 = _dev(flip1, torch.int32, "flip1")
     if out_bits is None:
-        out_bits = torch.empty((desc1.N, Hp, Wp, words(desc1.F)), dtype=torch.int32,
-                               device=x.device)
+        out_bits = _empty(x, (desc1.N, Hp, Wp, words(desc1.F)), torch.int32, stream)
     _dev(w1prep, torch.uint8, "w1prep")
     _check(lib.bnn_fconv_bconv2d(ctypes.byref(desc0), ctypes.byref(desc1), _ptr(x), _ptr(w0),
                                  _ptr(thr0), _ptr(flip0), _ptr(w1), _ptr(w1prep), _ptr(thr1),
@@ -448,8 +463,7 @@ def bnn_input_bconv_bconv2d(desc0: ConvDesc, desc1: ConvDesc, mode, x, offset, w
     flip0 = _dev(flip0, torch.int32, "flip0")
     flip1 = _dev(flip1, torch.int32, "flip1")
     if out_bits is None:
-        out_bits = torch.empty((desc1.N, Hp, Wp, words(desc1.F)), dtype=torch.int32,
-                               device=x.device)
+        out_bits = _empty(x, (desc1.N, Hp, Wp, words(desc1.F)), torch.int32, stream)
     _dev(w1prep, torch.uint8, "w1prep")
     _check(lib.bnn_input_bconv_bconv2d(ctypes.byref(desc0), ctypes.byref(desc1), int(mode),
                                        _ptr(x), _ptr(offset), _ptr(w0), _ptr(thr0), _ptr(flip0),
@@ -473,8 +487,7 @@ def bnn_bconv_bconv2d(desc0: ConvDesc, desc1: ConvDesc, x, w0, thr0, flip0, w1, 
     flip0 = _dev(flip0, torch.int32, "flip0")
     flip1 = _dev(flip1, torch.int32, "flip1")
     if out_bits is None:
-        out_bits = torch.empty((desc1.N, Hp, Wp, words(desc1.F)), dtype=torch.int32,
-                               device=x.device)
+        out_bits = _empty(x, (desc1.N, Hp, Wp, words(desc1.F)), torch.int32, stream)
     _check(lib.bnn_bconv_bconv2d(ctypes.byref(desc0), ctypes.byref(desc1), _ptr(x), _ptr(w0),
                                  _ptr(thr0), _ptr(flip0), _ptr(w1), _ptr(thr1), _ptr(flip1),
                                  _ptr(out_bits), _stream(stream)))
@@ -497,7 +510,7 @@ def bnn_bfc_pair(A, K0, w0, thr0, flip0, w1, N1, thr1=None, flip1=None, out=None
     thr1 = _dev(thr1, torch.int32, "thr1")
     flip1 = _dev(flip1, torch.int32, "flip1")
     if out is None:
-        out = torch.empty((M, N1) if thr1 is None else (M, 1), dtype=torch.int32, device=A.device)
+        out = _empty(A, (M, N1) if thr1 is None else (M, 1), torch.int32, stream)
     _check(lib.bnn_bfc_pair(M, K0, N0, N1, _ptr(A), _ptr(w0), _ptr(thr0), _ptr(flip0), _ptr(w1),
                             _ptr(thr1), _ptr(flip1), _ptr(out) if thr1 is None else None,
                             None if thr1 is None else _ptr(out), _stream(stream)))
@@ -519,7 +532,7 @@ def bnn_bfc_tail(A, K0, w0, thr0, flip0, w1, N1, accum, thr1=None, flip1=None, o
     thr1 = _dev(thr1, torch.int32, "thr1")
     flip1 = _dev(flip1, torch.int32, "flip1")
     if out is None:
-        out = torch.empty((M, N1) if thr1 is None else (M, 1), dtype=torch.int32, device=A.device)
+        out = _empty(A, (M, N1) if thr1 is None else (M, 1), torch.int32, stream)
     _check(lib.bnn_bfc_tail(M, K0, N0, N1, _ptr(A), _ptr(w0), _ptr(thr0), _ptr(flip0), _ptr(w1),
                             _ptr(thr1), _ptr(flip1), _ptr(out) if thr1 is None else None,
                             None if thr1 is None else _ptr(out), _ptr(accum), _stream(stream)))
@@ -542,9 +555,9 @@ def bnn_bgemm(A, B, K, thr=None, flip=None, want_sums=True, want_bits=True, out_
     thr = _dev(thr, torch.int32, "thr")
     flip = _dev(flip, torch.int32, "flip")
     if want_sums and out_sums is None:
-        out_sums = torch.empty((M, N), dtype=torch.int32, device=A.device)
+        out_sums = _empty(A, (M, N), torch.int32, stream)
     if want_bits and out_bits is None:
-        out_bits = torch.empty((M, words(N)), dtype=torch.int32, device=A.device)
+        out_bits = _empty(A, (M, words(N)), torch.int32, stream)
     _check(lib.bnn_bgemm(M, N, K, _ptr(A), _ptr(B), _ptr(thr), _ptr(flip), _ptr(out_sums),
                          _ptr(out_bits), _stream(stream)))
     return out_sums, out_bits
@@ -565,26 +578,6 @@ def _real(dtype, name):
 def _shaped(t, shape, name):
     if t is not None and t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, shape, tuple(t.shape)))
-    return t
-
-
-# A call's memory belongs to the stream that the call runs on (new_empty of a
-# tensor on the current one): torch's allocator may hand the block to other work
-# of that stream as soon as the tensor is dropped, and to no other's.
-def _scratch(like, shape, dtype, stream):
-    """A new tensor on like's device for the call alone."""
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
-
-
-def _empty(like, shape, dtype, stream):
-    """A new tensor on like's device that the caller gets, and may use and drop
-    on the current stream."""
-    t = _scratch(like, shape, dtype, stream)
-    if stream is not None:
-        t.record_stream(torch.cuda.current_stream(like.device))
     return t
 
 
@@ -822,10 +815,12 @@ def bnn_forward(net: Network, x, workspace=None, logits=None, stream=None):
     _dev(x, torch.float32, "x")
     batch = x.shape[0]
     if workspace is None:
-        workspace = net.alloc_workspace(batch, x.device)
+        # (zeroed on the stream that reads it)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            workspace = net.alloc_workspace(batch, x.device)
     n_out = net.layers[net.n - 1].N
     if logits is None:
-        logits = torch.empty((batch, n_out), dtype=torch.int32, device=x.device)
+        logits = _empty(x, (batch, n_out), torch.int32, stream)
     _check(lib.bnn_forward(net.layers, net.n, batch, net.H, net.W, net.C, _ptr(x),
                            _ptr(workspace), workspace.numel(), _ptr(logits),
                            _stream(stream)))
@@ -841,7 +836,7 @@ def bnn_forward_noalloc(net: Network, x, logits=None, stream=None):
     batch = x.shape[0]
     n_out = net.layers[net.n - 1].N
     if logits is None:
-        logits = torch.empty((batch, n_out), dtype=torch.int32, device=x.device)
+        logits = _empty(x, (batch, n_out), torch.int32, stream)
     _dev(logits, torch.int32, "logits")
     _check(lib.bnn_forward_noalloc(net.layers, net.n, batch, net.H, net.W, net.C, _ptr(x),
                                    _ptr(logits), _stream(stream)))

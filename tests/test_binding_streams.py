@@ -23,12 +23,16 @@ class Device(torch.Tensor):
     def new_empty(self, *size, **kw):
         return _made(torch.empty(*size, **kw))
 
+    def zero_(self):
+        _zeroed.append(_streams[-1].name)
+        return super().zero_()
+
     def record_stream(self, stream):
         self.held.append(stream.name)
 
 
 _streams = [CURRENT]
-_allocated = []
+_allocated, _zeroed = [], []
 
 
 def _made(t):
@@ -45,7 +49,7 @@ class Library:
         self.real, self.calls = real, []
 
     def __getattr__(self, name):
-        if name.endswith("_size") or name == "bnn_last_error":
+        if name.endswith(("_size", "_dims")) or name == "bnn_last_error":
             return getattr(self.real, name)
 
         def call(*args):
@@ -68,6 +72,7 @@ def lib(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _streams[-1])
     monkeypatch.setattr(torch, "empty", _host_empty)
     _allocated.clear()
+    _zeroed.clear()
     return fake
 
 
@@ -107,8 +112,85 @@ def _lora(**kw):
                        _t(2, 40, 8, dtype=f), **kw)
 
 
+def _conv(**kw):
+    bnn.bnn_bconv2d(bnn.conv_desc(1, 8, 8, 32, 32), _t(64), _t(9, 32), **kw)
+
+
+def _conv_prepared(**kw):
+    bnn.bnn_bconv2d_prepared(bnn.conv_desc(1, 8, 8, 32, 32), _t(64), _t(9, 32),
+                             _t(8, dtype=torch.uint8), **kw)
+
+
+def _prepare(**kw):
+    bnn.bnn_prepare_weights(_t(64, 3, 3, 2), 64, 3, 3, 64, **kw)
+
+
+def _first(**kw):
+    bnn.bnn_fconv2d_binw(bnn.conv_desc(1, 8, 8, 3, 32), _t(192, dtype=torch.float32), _t(9, 32), **kw)
+
+
+def _conv_input(**kw):
+    bnn.bnn_bconv2d_input(bnn.conv_desc(1, 8, 8, 3, 32), bnn.INPUT_THRESHOLD,
+                          _t(192, dtype=torch.float32), None, _t(9, 32), **kw)
+
+
+def _pair_desc():
+    return bnn.conv_desc(1, 8, 8, 3, 32), bnn.conv_desc(1, 8, 8, 32, 32)
+
+
+def _first_pair(**kw):
+    bnn.bnn_fconv_bconv2d(*_pair_desc(), _t(192, dtype=torch.float32), _t(288), _t(32), None, _t(288),
+                          _t(32), **kw)
+
+
+def _input_pair(**kw):
+    bnn.bnn_input_bconv_bconv2d(*_pair_desc(), bnn.INPUT_THRESHOLD, _t(192, dtype=torch.float32),
+                                None, _t(288), _t(32), None, _t(288), _t(32), **kw)
+
+
+def _conv_pair(**kw):
+    bnn.bnn_bconv_bconv2d(*_pair_desc(), _t(64), _t(288), _t(32), None, _t(288), _t(32), **kw)
+
+
+def _binarize(**kw):
+    bnn.bnn_binarize_input(bnn.INPUT_THRESHOLD, _t(1, 8, 8, 3, dtype=torch.float32), **kw)
+
+
+def _pack(**kw):
+    bnn.bnn_pack_bits(_t(5, 40, dtype=torch.float32), **kw)
+
+
+def _fc(**kw):
+    bnn.bnn_bgemm(_t(4, 2), _t(40, 2), 64, **kw)
+
+
+def _fc_pair(**kw):
+    bnn.bnn_bfc_pair(_t(4, 2), 64, _t(40, 2), _t(40), None, _t(8, 2), 8, **kw)
+
+
+def _fc_tail(**kw):
+    bnn.bnn_bfc_tail(_t(4, 2), 64, _t(40, 2), _t(40), None, _t(8, 2), 8, _t(8), **kw)
+
+
+def _net():
+    return bnn.Network([dict(kind=bnn.LAYER_INPUT_THRESHOLD, C=32, offset=_t(32, dtype=torch.float32)),
+                        dict(kind=bnn.LAYER_BFC_LOGITS, K=64 * 32, N=4, w=_t(4, 64))],
+                       8, 8, 32)
+
+
+def _forward(**kw):
+    bnn.bnn_forward(_net(), _t(2, 8, 8, 32, dtype=torch.float32), **kw)
+
+
+def _forward_noalloc(**kw):
+    bnn.bnn_forward_noalloc(_net(), _t(2, 8, 8, 32, dtype=torch.float32), **kw)
+
+
 CALLS = {  # outputs, workspaces
     _route: (2, 0), _group: (2, 1), _experts_fc: (1, 0), _experts_sum: (1, 1), _lora: (1, 1),
+    _conv: (2, 0), _conv_prepared: (2, 0), _prepare: (1, 0), _first: (2, 0), _conv_input: (2, 0),
+    _first_pair: (1, 0), _input_pair: (1, 0), _conv_pair: (1, 0), _binarize: (1, 0), _pack: (1, 0),
+    _fc: (2, 0), _fc_pair: (1, 0), _fc_tail: (1, 0), _forward: (1, 1), _forward_noalloc: (1, 0),
 }
 
 
@@ -120,6 +202,7 @@ def test_memory_of_the_stream_that_the_call_runs_on(lib, call):
     assert {t.on for t in _allocated} == {"other"}
     held = [t.held for t in _allocated]
     assert held.count(["current"]) == outputs and held.count([]) == workspaces
+    assert _zeroed == ["other"] * (call is _forward)  # its accumulators
     (_, args), = lib.calls
     assert args[-1] == OTHER.cuda_stream
 
