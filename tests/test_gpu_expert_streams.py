@@ -9,13 +9,18 @@ from paper_1808_00209_amd import bnn
 
 pytestmark = pytest.mark.gpu
 
+GROUP = 200001, 300              # M, G
+SUM = 1500, 2, 4, 1000, 700      # T, top_k, E, K, N
+LORA_FEW = 64, 512, 600, 5, 8    # M, K, N, adapters, rank
+LORA_MANY = 2100, 512, 600, 5, 8
+
 
 def _words(g, *shape):
     return torch.from_numpy(g.integers(-2 ** 31, 2 ** 31, size=shape).astype(np.int32)).cuda()
 
 
 def _group(seed):
-    M, G = 200001, 300
+    M, G = GROUP
     assert bnn.bnn_group_rows_workspace_size(M, G) > 0
     g = np.random.default_rng(seed)
     ids = torch.from_numpy(g.integers(-1, G, size=M).astype(np.int32)).cuda()
@@ -23,7 +28,7 @@ def _group(seed):
 
 
 def _experts_sum(seed):
-    T, k, E, K, N = 1500, 2, 4, 1000, 700
+    T, k, E, K, N = SUM
     assert bnn.bnn_experts_sum_workspace_size(bnn.ExpertsDesc(T, k, E, N, K, 1)) > 0
     g = np.random.default_rng(seed)
     ids = torch.from_numpy(g.integers(0, E, size=(T, k)).astype(np.int32)).cuda()
@@ -33,9 +38,9 @@ def _experts_sum(seed):
     return lambda **kw: (bnn.bnn_experts_sum(x, K, w, ids, weights, offsets, order, **kw),)
 
 
-def _lora(M):
+def _lora(sizes):
     def prepare(seed):
-        K, N, L, rank = 512, 600, 5, 8
+        M, K, N, L, rank = sizes
         assert bnn.bnn_bgemm_lora_workspace_size(bnn.LoraDesc(M, N, K, L, rank, 2, 2)) > 0
         g = torch.Generator(device="cuda").manual_seed(seed)
         r = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
@@ -46,7 +51,7 @@ def _lora(M):
     return prepare
 
 
-@pytest.mark.parametrize("prepare", [_group, _experts_sum, _lora(64), _lora(2100)],
+@pytest.mark.parametrize("prepare", [_group, _experts_sum, _lora(LORA_FEW), _lora(LORA_MANY)],
                          ids=["group", "experts_sum", "lora_few", "lora_many"])
 def test_two_streams_at_once(prepare):
     calls = [prepare(seed) for seed in (1, 2)]
