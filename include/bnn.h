@@ -630,8 +630,9 @@ typedef struct bnn_lora_desc {
  *   u[m][r] = sum_k x[m][k] * a[l][r][k],   l = ids[m];
  * a row whose id is not in [0, adapters) has the first term only.  Products
  * with u and their sums are held in fp32 or better and y is rounded once.
- * x must be finite; with one that is not, its row of y is unspecified (other
- * rows are not touched by it).
+ * A row's x, and a[l], b[l] and scale[l] of its adapter, must be finite; with
+ * one that is not, the row of y is unspecified.  Other rows are not touched by
+ * it: those of other adapters, and those without one, keep their bits.
  *   x        [M][K], rows x_stride elements apart (x_stride >= K).
  *   offset   [K] fp32 or NULL (0).
  *   w        [N][Kw] u32 packed weights.   alpha [N] fp32 or NULL (1).

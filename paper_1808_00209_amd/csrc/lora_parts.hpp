@@ -78,15 +78,20 @@ __device__ __forceinline__ void split_b(const RawB<T>& x, bool keep, v8bf (&out)
   }
 }
 
-// acc (32 outputs x 32 rows) += 16 ranks of b u^T, the smallest products first.
+// acc (32 outputs x 32 rows) += 16 ranks of b u^T, the smallest products first,
+// in the rows (a lane's sums are of one) that are `mine`; the others keep
+// theirs, whatever b and their u hold.
 template <class T>
-__device__ __forceinline__ void add_parts(v16f& acc, const v8bf (&b)[kParts<T>],
-                                          const v8bf (&u)[3]) {
+__device__ __forceinline__ void add_rows(v16f& acc, const v8bf (&b)[kParts<T>],
+                                         const v8bf (&u)[3], bool mine) {
+  v16f sum = acc;
 #pragma unroll
   for (int i = kParts<T> - 1; i >= 0; --i)
 #pragma unroll
     for (int j = 2; j >= 0; --j)
-      if (i + j < 4) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[i], u[j], acc, 0, 0, 0);
+      if (i + j < 4) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[i], u[j], sum, 0, 0, 0);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = mine ? sum[e] : acc[e];
 }
 
 }  // namespace bnn

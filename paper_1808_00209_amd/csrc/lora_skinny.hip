@@ -164,13 +164,14 @@ __global__ __launch_bounds__(64 * NW) void lora_up_skinny_kernel(UsArgs g) {
   v16f low = {};
   for (int r = 0; have && r < a.rank;) {
     const bool in = r + 8 * h < a.rank;
+    v8bf uf[3];
+    split_frag<3>(v, in, uf);
 #pragma unroll
     for (int i = 0; i < kAdapters; ++i) {
       if (l[i] < 0) continue;
-      v8bf bf[kParts<T>], uf[3];
+      v8bf bf[kParts<T>];
       split_b<T>(b[i], in && n0 + c < a.N, bf);
-      split_frag<3>(v, in && id == l[i], uf);
-      add_parts<T>(low, bf, uf);
+      add_rows<T>(low, bf, uf, id == l[i]);
     }
     if (!todo) {
       r += 16;

@@ -52,19 +52,6 @@ __device__ __forceinline__ Frag<T> load_frag(const T* p, int left) {
   return f;
 }
 
-// f where mask is ~0, zeros where it is 0.
-template <class T>
-__device__ __forceinline__ Frag<T> masked(const Frag<T>& f, uint32_t mask) {
-  constexpr int kWords = sizeof(Frag<T>) / 4;
-  uint32_t w[kWords];
-  __builtin_memcpy(w, f.v, sizeof(w));
-#pragma unroll
-  for (int i = 0; i < kWords; ++i) w[i] &= mask;
-  Frag<T> r;
-  __builtin_memcpy(r.v, w, sizeof(w));
-  return r;
-}
-
 // Lane 16 q + I's v in every lane of its row of 16 (DPP row_newbcast, taken by
 // the instruction that uses it).
 template <int I>
@@ -187,17 +174,25 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
       }
     }
   };
+  // A lane's sums are those of one row: they take an adapter's products where
+  // the row is the adapter's, and keep theirs else (as zeros in the product
+  // other rows would take 0 x infinity).
   auto multiply = [&](const Xs& x, const As& w, int d) {
     const uint32_t rows = adapter_rows[d];
 #pragma unroll
-    for (int i = 0; i < kDownRW; ++i) {
-      const uint32_t mine = (rows >> (16 * i + c)) & 1 ? ~0u : 0u;
+    for (int n = 0; n < NR; ++n) {
+      v4f sum[kDownRW];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const Frag<T> xm = masked(x[s][i], mine);
+      for (int i = 0; i < kDownRW; ++i) sum[i] = acc[i][n];
 #pragma unroll
-        for (int n = 0; n < NR; ++n) acc[i][n] = mma16(w[s][n], xm, acc[i][n]);
-      }
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int i = 0; i < kDownRW; ++i) sum[i] = mma16(w[s][n], x[s][i], sum[i]);
+#pragma unroll
+      for (int i = 0; i < kDownRW; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc[i][n][e] = (rows >> (16 * i + c)) & 1 ? sum[i][e] : acc[i][n][e];
     }
   };
   // The offsets of a group, an element per lane and load: lane (q, c) has
@@ -345,12 +340,12 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
     return (static_cast<uint32_t>(min(m00 + (tid >> 1), a.M - 1)) * g.Kw + 4 * (tid & 1)) * 4;
   });
 
-  // y = alpha S + u b^T, 32 rows after another.  u b^T takes 16 ranks at a time
-  // and one adapter of the rows after another, the rows of other adapters
-  // entering as zeros, in sums of its own (S is exact: so alpha S is rounded
-  // once, whatever the adapters add up).  While one such step multiplies, the
-  // next one's values are loaded, the next rows' first step among them.  A
-  // row's outputs leave through LDS (a region per wave) as one run.
+  // y = alpha S + u b^T, 32 rows after another.  u b^T takes 16 ranks at a time,
+  // and of these one adapter of the rows after another, in sums of its own (S
+  // is exact: so alpha S is rounded once, whatever the adapters add up).  While
+  // one such step multiplies, the next one's values are loaded, the next rows'
+  // first step among them.  A row's outputs leave through LDS (a region per
+  // wave) as one run.
   constexpr int kV = 16 / sizeof(Y);    // outputs per 16-byte store
   constexpr int kLanes = 64 / kV;       // lanes per row
   constexpr int kStride = 64 + kV;      // LDS outputs per row of 64
@@ -369,12 +364,10 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
 
   RawB<T> nb[2];
   float nu[8];
-  auto fetch = [&](int l, int r, int mine, int p) {
+  auto fetch_u = [&](int mine, int p, int r) {  // (mine < 0: other values)
     const int rr = r + 8 * h;
-#pragma unroll
-    for (int tf = 0; tf < 2; ++tf) nb[tf] = load_b<T>(a, l, f0 + 32 * tf + c, rr);
-    const bool in = mine == l && rr < a.rank;
-    const float* src = g.u + (in ? static_cast<size_t>(p) * a.rank + rr : size_t{0});
+    const float* src =
+        g.u + (mine >= 0 && rr < a.rank ? static_cast<size_t>(p) * a.rank + rr : size_t{0});
     __builtin_memcpy(nu, __builtin_assume_aligned(src, 16), sizeof(nu));
     for (int s = 1; s < g.slices; ++s) {
       float w[8];
@@ -384,41 +377,47 @@ __global__ __launch_bounds__(kTileNT, 2) void lora_up_kernel(UpArgs g) {
       for (int e = 0; e < 8; ++e) nu[e] += w[e];
     }
   };
-  auto waiting = [&](int pt) { return static_cast<uint32_t>(__ballot(id[pt] >= 0)); };
-  auto first_of = [&](int pt, uint32_t rows) {
-    return __builtin_amdgcn_readlane(id[pt], __builtin_ctz(rows));
+  auto fetch_b = [&](int tf, int l, int r) {
+    nb[tf] = load_b<T>(a, l, f0 + 32 * tf + c, r + 8 * h);
   };
-  if (const uint32_t rows = waiting(0)) fetch(first_of(0, rows), 0, id[0], base);
+  auto waiting = [&](int pt) { return static_cast<uint32_t>(__ballot(id[pt] >= 0)); };
+  // The first step of rows pt.
+  auto fetch_first = [&](int pt, uint32_t rows) {
+    const int l = __builtin_amdgcn_readlane(id[pt], __builtin_ctz(rows));
+    fetch_b(0, l, 0);
+    fetch_b(1, l, 0);
+    fetch_u(id[pt], base + 32 * pt, 0);
+  };
+  if (const uint32_t rows = waiting(0)) fetch_first(0, rows);
 #pragma unroll
   for (int pt = 0; pt < PT; ++pt) {
     asm volatile("" ::: "memory");  // (no loads of later rows up here: registers)
-    uint32_t todo = waiting(pt);
-    const uint32_t next_rows = pt + 1 < PT ? waiting(pt + 1 < PT ? pt + 1 : pt) : 0u;
-    auto fetch_next_rows = [&] {
-      if (pt + 1 < PT && next_rows) {
-        const int q = pt + 1 < PT ? pt + 1 : pt;
-        fetch(first_of(q, next_rows), 0, id[q], base + 32 * q);
-      }
-    };
+    const int np = pt + 1 < PT ? pt + 1 : pt;
+    const uint32_t rows = waiting(pt), next_rows = np > pt ? waiting(np) : 0u;
     v16f low[2] = {};
-    if (!todo) fetch_next_rows();
-    while (todo) {
-      const int l = first_of(pt, todo);
-      todo &= ~static_cast<uint32_t>(__ballot(id[pt] == l));
-      for (int r = 0; r < a.rank; r += 16) {
-        v8bf b[2][kParts<T>], u[3];
+    if (!rows && next_rows) fetch_first(np, next_rows);
+    for (int r = 0; rows && r < a.rank; r += 16) {
+      v8bf u[3];
+      split_frag<3>(nu, r + 8 * h < a.rank, u);
+      for (uint32_t todo = rows; todo;) {
+        const int l = __builtin_amdgcn_readlane(id[pt], __builtin_ctz(todo));
+        todo &= ~static_cast<uint32_t>(__ballot(id[pt] == l));
+        // The next step: another adapter, 16 ranks more, or the next rows.
+        const bool last = !todo && r + 16 >= a.rank;
+        const uint32_t from = todo ? todo : last ? next_rows : rows;
+        const int whose = last ? id[np] : id[pt];
+        const int nr = todo ? r : last ? 0 : r + 16;
+        const int nl = from ? __builtin_amdgcn_readlane(whose, __builtin_ctz(from)) : 0;
 #pragma unroll
-        for (int tf = 0; tf < 2; ++tf)
-          split_b<T>(nb[tf], f0 + 32 * tf + c < a.N && r + 8 * h < a.rank, b[tf]);
-        split_frag<3>(nu, id[pt] == l && r + 8 * h < a.rank, u);
-        if (r + 16 < a.rank)
-          fetch(l, r + 16, id[pt], base + 32 * pt);
-        else if (todo)
-          fetch(first_of(pt, todo), 0, id[pt], base + 32 * pt);
-        else
-          fetch_next_rows();
-#pragma unroll
-        for (int tf = 0; tf < 2; ++tf) add_parts<T>(low[tf], b[tf], u);
+        for (int tf = 0; tf < 2; ++tf) {
+          v8bf b[kParts<T>];
+          split_b<T>(nb[tf], f0 + 32 * tf + c < a.N && r + 8 * h < a.rank, b);
+          if (from) fetch_b(tf, nl, nr);
+          if (tf == 1 && from && !todo) fetch_u(whose, base + 32 * (last ? np : pt), nr);
+          add_rows<T>(low[tf], b, u, id[pt] == l);
+          // (one tile's sums at a time: both take registers that spill)
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
     // Register e of a tile holds output 8 (e / 4) + 4 h + e % 4 of row c.
