@@ -61,9 +61,9 @@ __device__ __forceinline__ float of_row_lane(float v) {
 }
 
 // The signs of 8 sums x + off as a byte, element 0 in bit 7.  off's values are
-// those of lanes 8 P .. 8 P + 7 of the row.  A finite sum is above 0 where its
-// pattern is, as a whole number (it is not -0: off has none); then 0 - pattern
-// has the sign bit.
+// those of lanes 8 P .. 8 P + 7 of the row.  A sum that is not NaN is above 0
+// where its pattern is, as a whole number (it is not -0: off has none); then 0 -
+// pattern has the sign bit.
 template <int P, class T>
 __device__ __forceinline__ uint32_t sign_byte(const Frag<T>& x, float off) {
   uint32_t byte = 0;
@@ -211,7 +211,8 @@ __global__ __launch_bounds__(kDownNT) void lora_down_kernel(LoraArgs a, float* _
     uint32_t w[kDownRW][4];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const float o = off[j] + 0.0f;  // -0 to +0
+      // -0 to +0; NaN, whose sum reads -1, to an infinity that does as well
+      const float o = off[j] == off[j] ? off[j] + 0.0f : -INFINITY;
 #pragma unroll
       for (int i = 0; i < kDownRW; ++i) {
         w[i][2 * j] = sign_byte<0>(x[2 * j][i], o) << (24 - 8 * q);
