@@ -517,9 +517,9 @@ typedef struct bnn_route_desc {
  * key is -inf or NaN (a logit of +inf counts as the largest finite value, a
  * finite one keeps its expert in reach, the type's lowest value too); it adds
  * nothing to the softmax's sum.  With groups > 1, a group's score is the sum
- * of its group_top largest keys (fewer in reach: their sum; none: lowest of
- * all), and only the experts of the top_groups groups of the largest scores
- * stay in reach.  ids[t] are the top_k experts of the largest keys in
+ * of its group_top largest keys (fewer in reach: their sum, which is not below
+ * the lowest finite value; none: lowest of all), and only the experts of the
+ * top_groups groups of the largest scores stay in reach.  ids[t] are the top_k experts of the largest keys in
  * descending order; equal keys, and equal group scores, go to the lowest
  * index.  weights[t][j] = scale * p of expert ids[t][j], divided by the sum
  * of the row's chosen p with renorm (0 where that sum is 0).  Where fewer

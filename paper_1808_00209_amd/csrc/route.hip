@@ -207,7 +207,8 @@ __global__ __launch_bounds__(kNT) void route_kernel(RouteArgs a) {
           b0 = larger(b0, v);
         }
       }
-      scores[g] = a.group_top == 2 && b1 > kNone ? b0 + b1 : b0;
+      // (-inf is the score of a group without any key in reach)
+      scores[g] = a.group_top == 2 && b1 > kNone ? fmaxf(b0 + b1, -FLT_MAX) : b0;
     }
     __syncthreads();
     // A group is kept where fewer than top_groups come before it.
