@@ -644,7 +644,7 @@ typedef struct bnn_lora_desc {
  *            one adapter that are far apart are quicker with it.  Entries out
  *            of range are clamped into it.
  *   y        [M][N].
- *   workspace as for bnn_experts_sum.
+ *   workspace as for bnn_experts_sum; its size never falls as M grows.
  * M >= 0 (0 launches nothing), M < 2^24, N <= 65536, K <= 65536, M * ceil(N /
  * 64) <= 2^28.  x, w, a, b and y 16-byte aligned.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN,
  * BNN_ERR_UNSUPPORTED (rank), BNN_ERR_WORKSPACE, BNN_ERR_HIP.

@@ -108,6 +108,15 @@ inline int lora_down_slices(int64_t M, int64_t K, int64_t rank) {
   return static_cast<int>(want < most ? want : most);
 }
 
+// Rows of u, over its slices, that M rows or any fewer can come to: at most
+// (255 + blocks) / blocks slices of M <= 32 blocks rows, M + 255 x 32.
+inline int64_t lora_u_rows(int64_t M, int64_t K, int64_t rank) {
+  if (lora_down_by_rows(M, rank)) return M;
+  const int64_t most = (K + 1023) / 1024 * M;
+  const int64_t some = M + 255 * 32 / ((rank + 63) / 64);
+  return most < some ? most : some;
+}
+
 // K split over a workgroup per 32 x 32 tile (lora_skinny.hip) while they are
 // about three per compute unit (128 rows, 4096 -> 4096, many adapters 18.7 us,
 // in the larger tiles 33.6; one per 16 rows, rank 64 21.8 and 25.5; 256 rows 27.1

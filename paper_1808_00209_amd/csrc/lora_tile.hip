@@ -462,7 +462,8 @@ size_t u_bytes(int64_t M, int32_t K, int32_t rank) {
 }  // namespace
 
 size_t lora_tile_workspace(int64_t M, int32_t K, int32_t rank) {
-  return M == 0 ? 0 : u_bytes(M, K, rank) + static_cast<size_t>(M) * words_of(K) * 4;
+  return (static_cast<size_t>(lora_u_rows(M, K, rank)) * rank + static_cast<size_t>(M) * words_of(K)) *
+         4;
 }
 
 bool lora_tile_supported(const LoraArgs& a) {
