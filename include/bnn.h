@@ -544,8 +544,8 @@ bnn_status bnn_route(const bnn_route_desc* d, int64_t T, const void* logits,
  *            - 1 in ascending order, then from offsets[G] on the rows of no
  *            group, in ascending order.
  *   workspace (device, 16-byte aligned, ws_bytes >= the size that
- *            bnn_group_rows_workspace_size gives, which is 0 for few rows;
- *            needs no initialization).
+ *            bnn_group_rows_workspace_size gives, which is 0 for few rows and
+ *            never falls as M grows; needs no initialization).
  * 1 <= G <= BNN_MAX_EXPERTS, 0 <= M < 2^24 (M == 0 writes the offsets only).
  * Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_WORKSPACE, BNN_ERR_ALIGN (the
  * workspace), BNN_ERR_HIP.
@@ -599,7 +599,8 @@ bnn_status bnn_experts_fc(const bnn_experts_desc* d, const uint32_t* x,
  *   dtype    bnn_dtype of y: BNN_F32, BNN_F16 or BNN_BF16.
  *   y        [T][N].
  *   workspace (device, 16-byte aligned, ws_bytes >= the size that
- *            bnn_experts_sum_workspace_size gives; needs no initialization).
+ *            bnn_experts_sum_workspace_size gives, which never falls as T
+ *            grows; needs no initialization).
  * Sizes, alignment (x, w, y) and errors as for bnn_experts_fc, plus
  * BNN_ERR_WORKSPACE.
  */

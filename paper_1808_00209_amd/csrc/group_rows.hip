@@ -227,7 +227,9 @@ __global__ __launch_bounds__(kNT) void group_place_kernel(const int32_t* __restr
 
 size_t group_rows_workspace(int64_t M, int32_t G) {
   if (M <= kOneRows) return 0;
-  return static_cast<size_t>(chunk_count(static_cast<int32_t>(M))) * (G + 1) * sizeof(int32_t);
+  // (the chunks of M rows or of any fewer: longer ones are fewer again)
+  const int64_t steps = (M + kStep - 1) / kStep;
+  return static_cast<size_t>(steps < kMaxChunks ? steps : kMaxChunks) * (G + 1) * sizeof(int32_t);
 }
 
 hipError_t launch_group_rows(int64_t M, int32_t G, const int32_t* ids, int32_t* offsets,

@@ -38,6 +38,22 @@ def test_bgemm_lora(rank, K):
         assert n <= (M * (rank + bnn.words(K)) + 8160 * rank) * 4
 
 
+GROUP_ROWS = list(range(16000, 40000)) + list(range(40000, 1 << 24, 4099)) + [(1 << 24) - 1]
+GROUP_ROWS += [m for k in range(2, 65) for m in (k * 262144 - 1, k * 262144 + 1) if m < 1 << 24]
+
+
+@pytest.mark.parametrize("G", [1, 256, 1024])
+def test_group_rows(G):
+    rows = sorted(GROUP_ROWS)
+    sizes = _sizes(bnn.load().bnn_group_rows_workspace_size, lambda M: (M, G), rows)
+    _never_falls(sizes, rows)
+    for M, n in zip(rows, sizes):
+        if M > 16384:  # a count per chunk of at least 2048 rows and group
+            steps = (M + 2047) // 2048
+            chunk = 2048 * ((steps + 127) // 128)
+            assert n >= (M + chunk - 1) // chunk * (G + 1) * 4
+
+
 @pytest.mark.parametrize("N, K", [(1, 1), (700, 1000), (4096, 4096), (65536, 65535)])
 def test_experts_sum(N, K):
     most = min(1 << 16, (1 << 28) // (4 * ((N + 63) // 64)))
