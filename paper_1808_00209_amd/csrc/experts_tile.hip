@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kTileNT, 2) void experts_tile_kernel(EtArgs a) {
 
 bool experts_tile_supported(const ExpertsArgs& a) {
   const int64_t kw = words_of(a.K);
-  return a.K < (1 << 22) && a.M / a.share * kw * 4 < (int64_t{1} << 32) - 64;
+  return a.M / a.share * kw * 4 < (int64_t{1} << 32) - 64;
 }
 
 hipError_t launch_experts_tile(const ExpertsArgs& a, uint16_t* counts, hipStream_t s) {
