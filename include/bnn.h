@@ -513,19 +513,21 @@ typedef struct bnn_route_desc {
  * Routing.  For row t and expert e, in fp32:
  *   z_e = logit_scale * logits[t][e];  p_e as in bnn_score;
  *   key_e = p_e + bias[e]  (bias NULL: key_e = p_e).
- * An expert is out of reach of the row where its logit is -inf or NaN, or its
- * key is -inf or NaN (a logit of +inf counts as the largest finite value, a
- * finite one keeps its expert in reach, the type's lowest value too); it adds
- * nothing to the softmax's sum.  With groups > 1, a group's score is the sum
- * of its group_top largest keys (fewer in reach: their sum, which is not below
- * the lowest finite value; none: lowest of all), and only the experts of the
- * top_groups groups of the largest scores stay in reach.  ids[t] are the top_k experts of the largest keys in
- * descending order; equal keys, and equal group scores, go to the lowest
- * index.  weights[t][j] = scale * p of expert ids[t][j], divided by the sum
- * of the row's chosen p with renorm (0 where that sum is 0).  Where fewer
- * than top_k experts are in reach (a padding row: none), the places left hold
- * id -1 and weight 0.  exp and the sums are in fp32, so keys that differ by
- * less than a few units in the last place may come in either order.
+ * z is held within the finite fp32 values (a logit of +inf: the largest one).
+ * An expert is out of reach of the row where its logit is -inf or NaN (a finite
+ * one keeps it in reach, the type's lowest value too) or its key is -inf or
+ * NaN.  One that its logit closes adds nothing to the softmax's sum; one that
+ * its bias closes does.  With groups > 1, a group's score is the sum of its
+ * group_top largest keys (fewer in reach: their sum, which is not below the
+ * lowest finite value; none: lowest of all), and only the experts of the
+ * top_groups groups of the largest scores stay in reach.  ids[t] are the top_k
+ * experts of the largest keys in descending order; equal keys, and equal group
+ * scores, go to the lowest index.  weights[t][j] = scale * p of expert
+ * ids[t][j], divided by the sum of the row's chosen p with renorm (0 where that
+ * sum is 0).  Where fewer than top_k experts are in reach (a padding row:
+ * none), the places left hold id -1 and weight 0.  exp and the sums are in
+ * fp32, so keys that differ by less than a few units in the last place may come
+ * in either order.
  *   logits  [T][E], rows `stride` elements apart (stride >= E), of d->dtype.
  *   bias    [E] fp32 or NULL.
  *   ids     [T][top_k] int32.   weights [T][top_k] fp32.
@@ -634,6 +636,8 @@ typedef struct bnn_lora_desc {
  * A row's x, and a[l], b[l] and scale[l] of its adapter, must be finite; with
  * one that is not, the row of y is unspecified.  Other rows are not touched by
  * it: those of other adapters, and those without one, keep their bits.
+ * With the same number of rows, a row's bits are the same whatever the order
+ * and the other rows; another number may add up u in another order.
  *   x        [M][K], rows x_stride elements apart (x_stride >= K).
  *   offset   [K] fp32 or NULL (0).
  *   w        [N][Kw] u32 packed weights.   alpha [N] fp32 or NULL (1).
@@ -647,8 +651,9 @@ typedef struct bnn_lora_desc {
  *   y        [M][N].
  *   workspace as for bnn_experts_sum; its size never falls as M grows.
  * M >= 0 (0 launches nothing), M < 2^24, N <= 65536, K <= 65536, M * ceil(N /
- * 64) <= 2^28.  x, w, a, b and y 16-byte aligned.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE, BNN_ERR_ALIGN,
- * BNN_ERR_UNSUPPORTED (rank), BNN_ERR_WORKSPACE, BNN_ERR_HIP.
+ * 64) <= 2^28.  x, w, a, b and y 16-byte aligned.  Errors: BNN_ERR_NULL,
+ * BNN_ERR_SHAPE, BNN_ERR_ALIGN, BNN_ERR_UNSUPPORTED (rank), BNN_ERR_WORKSPACE,
+ * BNN_ERR_HIP.
  */
 bnn_status bnn_bgemm_lora_workspace_size(const bnn_lora_desc* d, size_t* bytes);
 bnn_status bnn_bgemm_lora(const bnn_lora_desc* d, const void* x,

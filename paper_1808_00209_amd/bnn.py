@@ -2,9 +2,11 @@
 
 Argument marshalling only: every function checks tensor dtypes, devices and
 contiguity, allocates outputs with torch when the caller does not pass them,
-and calls the C entry point of the same name on the current HIP stream.  All
-computation happens in the library's HIP kernels.  Loading fails loudly when
-libbnn.so has not been built (``python -m paper_1808_00209_amd.build``).
+and calls the C entry point of the same name on the current HIP stream, or on
+the one given as ``stream``: what the call allocates is then memory of that
+stream.  All computation happens in the library's HIP kernels.  Loading fails
+loudly when libbnn.so has not been built
+(``python -m paper_1808_00209_amd.build``).
 """
 from __future__ import annotations
 

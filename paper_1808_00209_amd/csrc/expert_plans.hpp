@@ -50,9 +50,14 @@ TileShape tile_shape(int64_t N, int64_t chunks, double fixed, double tail, F row
 // ---------------------------------------------------------------- experts ---
 
 // bnn_experts_sum for few rows: every row reads its experts' weights by itself,
-// up to 32 MiB of them in all (experts_sum_rows.hip, one launch; rows x 8 of 64
-// experts, 4096 -> 1024, against products and combining pass: 4 rows 6.0 and
-// 13.1 us, 8 8.1 and 20.0, 32 28.5 and 21.3; 32 rows 1024 -> 1024 13.4 and 12.9).
+// up to 32 MiB of them in all (experts_sum_rows.hip, one launch; against
+// products and combining pass, 4096 -> 1024, rows x 8 of 64 experts: 4 rows 6.3
+// and 13.4 us, 8 8.4 and 14.6, 16 14.2 and 18.2, 32 27.2 and 18.3; 8 of 8: 8
+// rows 8.4 and 9.2, 16 14.4 and 9.4; 2 of 8: 32 rows 7.8 and 8.5, 64 12.2 and
+// 10.3; 1 of 2: 64 rows 7.4 and 8.4).  It does not look at the number of
+// experts: between the limit and twice it, the form taken loses 4 us with many,
+// and up to the limit 5 with few and short rows (8 of 8, 1024 -> 1024, 32 rows
+// 13.2 and 8.2).
 inline bool experts_sum_by_rows(int64_t M, int64_t N, int64_t K) {
   return M * N * ((K + 31) / 32) <= (int64_t{8} << 20);
 }
@@ -80,7 +85,11 @@ inline TileShape experts_shape(int64_t M, int64_t E, int64_t N, int64_t chunks) 
 // The combining pass (experts_combine.hip) stages the alphas of all experts for
 // 256 outputs in LDS (at most 64 KiB of them) where a block, two per compute
 // unit, has 64 rows or more: fewer do not pay for the staging.  Rows per block,
-// or 0 for the form that reads them as it goes.
+// or 0 for the form that reads them as it goes.  Staged and not, rows x experts
+// per row of E, outputs: 8192 x 8 of 64, 4096: 170 and 199 us; 3000 x 8 of 64,
+// 4096: 48 and 51; 8192 x 8 of 64, 1024: 37.6 and 36.0; 8192 x 2 of 64, 1024: 22
+// and 16; 32768 x 2 of 8, 512: 27 and 26.  Beyond 64 experts not, 35.6 us for
+// 8192 x 8 of 128 or 256, 1024.
 constexpr int kCombineCols = 256;
 inline int combine_rows(int64_t T, int64_t E, int64_t N) {
   const int64_t cols = (N + kCombineCols - 1) / kCombineCols;

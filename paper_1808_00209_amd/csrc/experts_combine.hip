@@ -7,9 +7,10 @@
 // A thread computes 8 outputs of a row.  The bytes are the counts, top_k N 2
 // per row, and y; but every pair also reads its expert's alpha, twice the
 // bytes of its counts, from the L2: 8192 rows x 8 experts, 1024 outputs, 122 us
-// with one read after another.  Many rows therefore stage the alphas of all
-// experts for 256 outputs in LDS (42 us, 168 MB at 4 TB/s); few have all their
-// reads in flight.
+// with one read after another.  Two forms avoid that: a row's reads are all in
+// flight (36 us, 168 MB at 4.6 TB/s, at 64, 128 and 256 experts), or the alphas
+// of all experts for 256 outputs are staged in LDS for many rows (combine_rows
+// in expert_plans.hpp).
 #include "dtypes.hpp"
 #include "expert_plans.hpp"
 #include "experts.hpp"

@@ -2,13 +2,14 @@
 // products of bnn_experts_sum): one GEMM tile of fp4_tile.hpp per row tile of
 // an expert and 64, 128 or 256 outputs, the rows gathered through the order.
 //
-// 65536 pairs of 64 experts, 1024 -> 4096 to bits: 129 us, 4.2e15 operations a
-// second; 4096 -> 1024 to counts 113-122 us (the FC kernel without experts
-// reaches 5.5e15 at the clock that load allows).  The difference is row tiles
-// that experts do not fill and each block's start and end, at 1024 bits as long
-// as its four chunks: there the matrix cores are busy in 47 % of the cycles, and
-// 6.3 vector instructions issue per MFMA.  One launch bound for all: the grid holds the most tiles
-// that there can be, blocks past the last one end at once.
+// 65536 pairs of 64 experts, 1024 -> 4096 to bits: 125-137 us from card to card,
+// 4.1e15 operations a second; 4096 -> 1024 to counts 113-122 us (the FC kernel
+// without experts reaches 5.5e15 at the clock that load allows).  The difference
+// is row tiles that experts do not fill and each block's start and end, at 1024
+// bits as long as its four chunks: there the matrix cores are busy in 47 % of
+// the cycles, and 6.3 vector instructions issue per MFMA.  One launch bound for
+// all: the grid holds the most tiles that there can be, blocks past the last one
+// end at once.
 #include "expert_plans.hpp"
 #include "experts.hpp"
 #include "fp4_tile.hpp"

@@ -123,7 +123,7 @@ __global__ __launch_bounds__(64 * NW) void lora_up_skinny_kernel(UsArgs g) {
   const int row = lora_row(a, p);
   const int id = p < a.M ? lora_adapter(a, row) : -1;
   // u b^T: 16 ranks of an adapter are a job of wave (adapter + ranks / 16) mod
-  // NW, so that a row's sums do not hang on the rows beside it.  The first
+  // NW, so that a row's sums do not hang on which rows lie beside it.  The first
   // jobs' values are loaded before the binary products.
   const uint32_t have = static_cast<uint32_t>(__ballot(id >= 0));
   float v[8];            // u, 16 ranks of the row
