@@ -756,7 +756,8 @@ def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=N
     _u32(w)
     N = w.shape[0]
     _shaped(w, (N, words(K)), "w")
-    _dev(a, kind, "a")
+    if _dev(a, kind, "a").dim() != 3:
+        raise ValueError("a must have shape [adapters, rank, %d], got %s" % (K, tuple(a.shape)))
     L, rank = a.shape[0], a.shape[1]
     _shaped(a, (L, rank, K), "a")
     _shaped(_dev(b, kind, "b"), (L, N, rank), "b")

@@ -46,3 +46,12 @@ def test_overlapping_rows_are_refused(overlapping):
         bnn.bnn_bgemm_lora(x, _on_device(torch.zeros((n, bnn.words(k)), dtype=torch.int32)),
                            _on_device(torch.zeros(x.shape[0], dtype=torch.int32)),
                            _on_device(torch.zeros(1, 8, k)), _on_device(torch.zeros(1, n, 8)))
+
+
+@pytest.mark.parametrize("shape", [(), (8,), (8, 64), (1, 8, 63), (1, 1, 8, 64)], ids=str)
+def test_adapters_of_another_shape_are_refused(shape):
+    x = _on_device(torch.zeros(4, 64))
+    with pytest.raises(ValueError, match="a must have shape"):
+        bnn.bnn_bgemm_lora(x, _on_device(torch.zeros((8, 2), dtype=torch.int32)),
+                           _on_device(torch.zeros(4, dtype=torch.int32)),
+                           _on_device(torch.zeros(shape)), _on_device(torch.zeros(1, 8, 8)))
