@@ -60,7 +60,7 @@
 extern "C" {
 #endif
 
-#define BNN_ABI_VERSION 9
+#define BNN_ABI_VERSION 10
 
 typedef enum bnn_status {
   BNN_OK = 0,
@@ -481,7 +481,7 @@ typedef enum bnn_dtype {
   BNN_F32 = 0,
   BNN_F16 = 1,
   BNN_BF16 = 2,
-  BNN_I32 = 3 /* int32 sums, e.g. of bnn_bgemm (bnn_route only) */
+  BNN_I32 = 3 /* int32 sums, e.g. of bnn_bgemm (logits only) */
 } bnn_dtype;
 
 typedef enum bnn_score {
@@ -662,6 +662,136 @@ bnn_status bnn_bgemm_lora(const bnn_lora_desc* d, const void* x,
                           const int32_t* ids, const void* a, const void* b,
                           const float* scale, const int32_t* order, void* y,
                           void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------- 8-bit layers and their answers -- */
+/*
+ * The layers of a binarized network that keep more than one bit: its first and
+ * last ones, and projections that lose too much as signs.  bnn_rmsnorm leaves
+ * 8-bit integers with a scale per row, bnn_q8gemm multiplies them with 8-bit
+ * weights that have a scale per output, and bnn_logprobs reads the answers from
+ * the last layer's logits (those of bnn_q8gemm, or bnn_bgemm's int32 sums).
+ * Not part of the paper.  Inference only: no call has a gradient.
+ */
+
+typedef struct bnn_rmsnorm_desc {
+  int64_t M;            /* rows                                              */
+  int32_t D;            /* values of a row, 1..BNN_MAX_NORM_SIZE             */
+  int32_t dtype;        /* of x, residual, sum and y: BNN_F32, BNN_F16 or    */
+                        /* BNN_BF16                                          */
+  int32_t weight_dtype; /* of weight: dtype or BNN_F32                       */
+  float eps;            /* >= 0 and finite                                   */
+} bnn_rmsnorm_desc;
+
+#define BNN_MAX_NORM_SIZE 65536
+
+/*
+ * Root-mean-square norm of the rows, with a residual added on the way:
+ *   h[m][d] = x[m][d] + residual[m][d], added in fp32 and rounded once to dtype
+ *             (residual NULL: x[m][d]),
+ *   y[m][d] = h[m][d] * r[m] * weight[d],
+ *   r[m]    = 1 / sqrt(sum_d h[m][d]^2 / D + eps)   (0 where that root is 0),
+ * and in 8 bits:
+ *   scale[m] = max_d |y[m][d]| / 127,   q[m][d] = y[m][d] / scale[m] rounded to
+ *   nearest, ties to even: -127..127 (all 0, and scale 0, in a row of zeros).
+ * r cancels in q, which is rounded from the exact h * weight: the same whatever
+ * the order of the sums.  r and scale are good to a few units of fp32, y is
+ * rounded once more to dtype.  A row whose h holds an infinity or NaN: scale
+ * and y NaN, q 0.  weight must be finite (or else q, scale and y of the rows
+ * are unspecified).
+ *   x        [M][D], rows x_stride elements apart (x_stride >= D).
+ *   residual [M][D], rows residual_stride elements apart, or NULL.
+ *   weight   [D] or NULL (1).
+ *   sum      [M][D] (h), or NULL.      y [M][D] or NULL.
+ *   q        [M][D] int8, rows q_stride bytes apart (q_stride >= D; what lies
+ *            between the rows is left as it is), or NULL.
+ *   scale    [M] fp32; NULL with q NULL, and only then.
+ * One of sum, y and q must be given.  sum or y (not both) may be x or residual
+ * itself where its rows are contiguous (stride D).  Rows need only be aligned
+ * to their element.  M >= 0 (0 launches nothing), M < 2^24.  Errors:
+ * BNN_ERR_NULL, BNN_ERR_SHAPE (also a pointer not aligned to its element),
+ * BNN_ERR_HIP.
+ */
+bnn_status bnn_rmsnorm(const bnn_rmsnorm_desc* d, const void* x,
+                       int64_t x_stride, const void* residual,
+                       int64_t residual_stride, const void* weight, void* sum,
+                       void* y, int8_t* q, int64_t q_stride, float* scale,
+                       hipStream_t stream);
+
+typedef struct bnn_q8gemm_desc {
+  int64_t M;         /* rows (tokens)                                        */
+  int32_t N, K;      /* outputs, inputs                                      */
+  int32_t dtype;     /* of y: BNN_F32, BNN_F16 or BNN_BF16                   */
+} bnn_q8gemm_desc;
+
+/*
+ * Matrix product of 8-bit integers:
+ *   y[m][n] = (S[m][n] * x_scale[m]) * w_scale[n] + bias[n],
+ *   S[m][n] = sum_k x[m][k] * w[n][k]   (exact, in int32: K <= 131071),
+ * S rounded to fp32, the products and the sum in fp32, y rounded once to dtype.
+ *   x        [M][K] int8, rows x_stride bytes apart (x_stride >= K).
+ *   x_scale  [M] fp32 or NULL (1).
+ *   w        [N][K] int8, rows w_stride bytes apart (w_stride >= K).
+ *   w_scale  [N] fp32 or NULL (1).    bias [N] fp32 or NULL (0).
+ *   y        [M][N].
+ * Values of -128 are as good as any.  Rows may lie anywhere; where x and w are
+ * 16-byte aligned and their strides a multiple of 16 (as bnn_rmsnorm's binding
+ * lays out q), large products are quicker.  What lies between the rows is never
+ * used.
+ * M >= 0 (0 launches nothing), M < 2^24, 1 <= N <= 2^20, 1 <= K <= 131071,
+ * M * N <= 2^35, strides <= 2^31.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE,
+ * BNN_ERR_ALIGN (y is not aligned to 16 bytes), BNN_ERR_HIP.
+ */
+bnn_status bnn_q8gemm(const bnn_q8gemm_desc* d, const int8_t* x,
+                      int64_t x_stride, const float* x_scale, const int8_t* w,
+                      int64_t w_stride, const float* w_scale,
+                      const float* bias, void* y, hipStream_t stream);
+
+typedef struct bnn_logprobs_desc {
+  int64_t T;         /* rows                                                 */
+  int32_t V;         /* answers (classes, tokens), 1..2^24                   */
+  int32_t n;         /* given answers per row, 0..BNN_MAX_GIVEN              */
+  int32_t top_k;     /* alternatives per row, 0..min(BNN_MAX_ALTERNATIVES,   */
+                     /* V)                                                   */
+  int32_t dtype;     /* bnn_dtype of the logits                              */
+  float logit_scale; /* factor on the logits (1 / temperature), positive and */
+                     /* finite                                               */
+} bnn_logprobs_desc;
+
+#define BNN_MAX_GIVEN 1024
+#define BNN_MAX_ALTERNATIVES 32
+
+/*
+ * Log probabilities of answers.  For row t, with z_v = logit_scale *
+ * logits[t][v] and p = softmax(z):
+ *   logp[t][j]     = ln p of answer ids[t][j] (-inf for an id not in [0, V)),
+ *   entropy[t]     = -sum_v p_v ln p_v,
+ *   top_ids[t][j], top_logp[t][j]   the top_k answers of the largest logits in
+ *                  descending order, equal ones (0 and -0 are) by the lowest
+ *                  index, and their ln p.
+ * A logit of -inf takes its answer out of reach: p 0, logp -inf, never among
+ * the alternatives (places left hold id -1 and -inf).  The type's lowest finite
+ * value is a value as any other.  In a row with nothing in reach every logp is
+ * -inf and the entropy 0.  A row that holds NaN or +inf: logp, entropy and
+ * top_logp NaN, top_ids -1 (-inf stays for ids not in [0, V)).  Sums are held
+ * in fp32.
+ *   logits  [T][V], rows `stride` elements apart (stride >= V), of d->dtype.
+ *   ids     [T][n] int32 and logp [T][n] fp32, or both NULL with n == 0.
+ *   entropy [T] fp32 or NULL.
+ *   top_ids [T][top_k] int32 and top_logp [T][top_k] fp32, or both NULL with
+ *           top_k == 0.
+ *   workspace (device, 16-byte aligned, ws_bytes >= the size that
+ *           bnn_logprobs_workspace_size gives for d, which never falls as T grows;
+ *           needs no initialization).
+ * T >= 0 (0 launches nothing), T < 2^24.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE
+ * (also logits not aligned to their element), BNN_ERR_WORKSPACE, BNN_ERR_ALIGN
+ * (the workspace), BNN_ERR_HIP.
+ */
+bnn_status bnn_logprobs_workspace_size(const bnn_logprobs_desc* d,
+                                       size_t* bytes);
+bnn_status bnn_logprobs(const bnn_logprobs_desc* d, const void* logits,
+                        int64_t stride, const int32_t* ids, float* logp,
+                        float* entropy, int32_t* top_ids, float* top_logp,
+                        void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------ layer chain */
 typedef enum bnn_layer_kind {

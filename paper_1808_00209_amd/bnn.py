@@ -44,6 +44,7 @@ EXPORTED = ["bnn_last_error", "bnn_abi_version", "bnn_default_options", "bnn_set
             "bnn_bgemm",
             "bnn_route", "bnn_group_rows_workspace_size", "bnn_group_rows", "bnn_experts_fc", "bnn_experts_sum_workspace_size",
             "bnn_experts_sum", "bnn_bgemm_lora_workspace_size", "bnn_bgemm_lora",
+            "bnn_rmsnorm", "bnn_q8gemm", "bnn_logprobs_workspace_size", "bnn_logprobs",
             "bnn_forward_workspace_size", "bnn_forward", "bnn_forward_noalloc"]
 
 # Bytes of bnn_forward_noalloc's per-GPU scratch array (BNN_FORWARD_SCRATCH_BYTES).
@@ -99,6 +100,22 @@ class LoraDesc(ctypes.Structure):
                                           ("N", "K", "adapters", "rank", "dtype", "out_dtype")]
 
 
+class RmsnormDesc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in
+                                          ("D", "dtype", "weight_dtype")]
+    _fields_ += [("eps", ctypes.c_float)]
+
+
+class Q8gemmDesc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("N", "K", "dtype")]
+
+
+class LogprobsDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in
+                                          ("V", "n", "top_k", "dtype")]
+    _fields_ += [("logit_scale", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -150,6 +167,12 @@ def load(path: str = LIB_PATH):
                                                   ctypes.POINTER(ctypes.c_size_t)]
     lib.bnn_bgemm_lora.argtypes = [ctypes.POINTER(LoraDesc), P, i64, P, P, P, P, P, P, P, P, P, P,
                                    ctypes.c_size_t, P]
+    lib.bnn_rmsnorm.argtypes = [ctypes.POINTER(RmsnormDesc), P, i64, P, i64, P, P, P, P, i64, P, P]
+    lib.bnn_q8gemm.argtypes = [ctypes.POINTER(Q8gemmDesc), P, i64, P, P, i64, P, P, P, P]
+    lib.bnn_logprobs_workspace_size.argtypes = [ctypes.POINTER(LogprobsDesc),
+                                                ctypes.POINTER(ctypes.c_size_t)]
+    lib.bnn_logprobs.argtypes = [ctypes.POINTER(LogprobsDesc), P, i64, P, P, P, P, P, P,
+                                 ctypes.c_size_t, P]
     lib.bnn_forward_workspace_size.argtypes = [ctypes.POINTER(Layer), i32, i32, i32, i32, i32,
                                                ctypes.POINTER(ctypes.c_size_t)]
     lib.bnn_forward.argtypes = [ctypes.POINTER(Layer), i32, i32, i32, i32, i32, P, P,
@@ -776,6 +799,147 @@ def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=N
                               _ptr(alpha), _ptr(ids), _ptr(a), _ptr(b), _ptr(scale), _ptr(order),
                               _ptr(out), _ptr(workspace), n, _stream(stream)))
     return out
+
+
+# ----------------------------------------- 8-bit layers and their answers ---
+def _together(like, *others):
+    """Every tensor of a call lies on the current device, like the stream."""
+    at = like.device
+    for t in others:
+        if t is not None and t.device != at:
+            raise ValueError("tensors on %s and on %s in one call" % (at, t.device))
+    if at.index is not None and _raw_device is not None and at.index != _raw_device():
+        raise ValueError("tensors on %s, but the current device is cuda:%d: use torch.cuda.device"
+                         % (at, _raw_device()))
+
+
+def _rows8(like, M, D, stream):
+    """New 8-bit rows [M, D], a multiple of 16 bytes apart."""
+    return _empty(like, (M, (D + 15) // 16 * 16), torch.int8, stream)[:, :D]
+
+
+def _int8_rows(t, name):
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int8:
+        raise TypeError("%s must be a CUDA(HIP) tensor of int8" % name)
+    return _rows(t, name)
+
+
+def bnn_rmsnorm(x, weight=None, residual=None, eps=1e-6, want_y=False, want_q=True, sum=None,
+                y=None, q=None, scale=None, stream=None):
+    """Root-mean-square norm: x, residual [M, D] (float32, float16 or bfloat16;
+    rows may be strided), weight [D] of x's type or float32 -> (h, y, q,
+    scale): h = x + residual [M, D] (None without a residual, unless ``sum`` is
+    given), y = h / sqrt(mean(h^2) + eps) * weight [M, D] of x's type (want_y),
+    and y in 8 bits (want_q): q [M, D] int8 in rows a multiple of 16 bytes
+    apart, scale [M] float32, y = q * scale.  ``sum`` or ``y`` may be x or
+    residual itself."""
+    lib = load()
+    kind = x.dtype
+    code = _real(kind, "x")
+    stride = _rows(x, "x")
+    M, D = x.shape
+    r_stride = 0
+    if residual is not None:
+        if residual.dtype is not kind:
+            raise TypeError("residual must be of x's type, %s" % kind)
+        r_stride = _rows(_shaped(residual, (M, D), "residual"), "residual")
+    w_code = code
+    if weight is not None:
+        w_code = 0 if weight.dtype is torch.float32 else code
+        _shaped(_dev(weight, kind if w_code else torch.float32, "weight"), (D,), "weight")
+    if residual is not None or sum is not None:
+        sum = _output(sum, x, (M, D), kind, "sum", stream)
+    if want_y or y is not None:
+        y = _output(y, x, (M, D), kind, "y", stream)
+    if want_q or q is not None:
+        if q is None:
+            q = _rows8(x, M, D, stream)
+        q_stride = _int8_rows(_shaped(q, (M, D), "q"), "q")
+        scale = _output(scale, x, (M,), torch.float32, "scale", stream)
+    elif scale is not None:
+        raise ValueError("scale goes with q")
+    else:
+        q_stride = 0
+    _together(x, residual, weight, sum, y, q, scale)
+    d = RmsnormDesc(M, D, code, w_code, eps)
+    _check(lib.bnn_rmsnorm(ctypes.byref(d), _ptr(x), stride, _ptr(residual), r_stride,
+                           _ptr(weight), _ptr(sum), _ptr(y), _ptr(q), q_stride, _ptr(scale),
+                           _stream(stream)))
+    return sum, y, q, scale
+
+
+def bnn_q8gemm(x, w, x_scale=None, w_scale=None, bias=None, dtype=torch.float32, out=None,
+               stream=None):
+    """8-bit matrix product: x [M, K], w [N, K] int8 (rows may be strided; the
+    quickest where they are a multiple of 16 bytes apart), x_scale [M],
+    w_scale [N], bias [N] float32 or None -> y [M, N] of dtype (float32,
+    float16 or bfloat16), y = (x . w) * x_scale[m] * w_scale[n] + bias[n]."""
+    lib = load()
+    x_stride, w_stride = _int8_rows(x, "x"), _int8_rows(w, "w")
+    M, K = x.shape
+    N = w.shape[0]
+    _shaped(w, (N, K), "w")
+    _shaped(_dev(x_scale, torch.float32, "x_scale"), (M,), "x_scale")
+    _shaped(_dev(w_scale, torch.float32, "w_scale"), (N,), "w_scale")
+    _shaped(_dev(bias, torch.float32, "bias"), (N,), "bias")
+    dtype = dtype if out is None else out.dtype
+    code = _real(dtype, "out")
+    out = _output(out, x, (M, N), dtype, "out", stream)
+    _together(x, w, x_scale, w_scale, bias, out)
+    d = Q8gemmDesc(M, N, K, code)
+    _check(lib.bnn_q8gemm(ctypes.byref(d), _ptr(x), x_stride, _ptr(x_scale), _ptr(w), w_stride,
+                          _ptr(w_scale), _ptr(bias), _ptr(out), _stream(stream)))
+    return out
+
+
+def bnn_logprobs_workspace_size(desc: LogprobsDesc) -> int:
+    out = ctypes.c_size_t()
+    _check(load().bnn_logprobs_workspace_size(ctypes.byref(desc), ctypes.byref(out)))
+    return out.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _logprobs_bytes(T, V, top_k):
+    return bnn_logprobs_workspace_size(LogprobsDesc(T, V, 0, top_k, 0, 1.0))
+
+
+def bnn_logprobs(logits, ids=None, top_k=0, logit_scale=1.0, want_entropy=True, logp=None,
+                 entropy=None, top_ids=None, top_logp=None, workspace=None, stream=None):
+    """Log probabilities of answers: logits [T, V] (float32, float16, bfloat16
+    or int32; rows may be strided), ids [T] or [T, n] int32 or None, p =
+    softmax(logit_scale * logits) -> (logp of ids' shape, entropy [T],
+    top_ids [T, top_k] int32, top_logp [T, top_k]), float32; None for what is
+    not asked for.  The top_k alternatives come in descending order, equal
+    logits by the lowest index; answers out of reach (logit -inf) have ln p
+    -inf and are no alternatives (id -1), as have ids not in [0, V)."""
+    lib = load()
+    dtype = _DTYPES.get(logits.dtype)
+    if dtype is None:
+        raise TypeError("logits must be float32, float16, bfloat16 or int32")
+    stride = _rows(logits, "logits")
+    T, V = logits.shape
+    n = 0
+    if ids is not None:
+        if _dev(ids, torch.int32, "ids").dim() not in (1, 2) or ids.shape[0] != T:
+            raise ValueError("ids must have shape (%d,) or (%d, n), got %s" % (T, T, tuple(ids.shape)))
+        n = ids.shape[1] if ids.dim() == 2 else 1
+        logp = _output(logp, logits, tuple(ids.shape), torch.float32, "logp", stream)
+    elif logp is not None:
+        raise ValueError("logp goes with ids")
+    if want_entropy or entropy is not None:
+        entropy = _output(entropy, logits, (T,), torch.float32, "entropy", stream)
+    if top_k:
+        top_ids = _output(top_ids, logits, (T, top_k), torch.int32, "top_ids", stream)
+        top_logp = _output(top_logp, logits, (T, top_k), torch.float32, "top_logp", stream)
+    elif top_ids is not None or top_logp is not None:
+        raise ValueError("top_ids and top_logp go with top_k")
+    d = LogprobsDesc(T, V, n, top_k, dtype, logit_scale)
+    workspace, size = _workspace(workspace, _logprobs_bytes(T, V, top_k), logits, stream)
+    _together(logits, ids, logp, entropy, top_ids, top_logp, workspace)
+    _check(lib.bnn_logprobs(ctypes.byref(d), _ptr(logits), stride, _ptr(ids), _ptr(logp),
+                            _ptr(entropy), _ptr(top_ids), _ptr(top_logp), _ptr(workspace), size,
+                            _stream(stream)))
+    return logp, entropy, top_ids, top_logp
 
 
 class Network:

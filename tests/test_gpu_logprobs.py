@@ -1,0 +1,216 @@
+"""Log probabilities of answers against their definition in 64 bits (quant_ref).
+
+Tolerances.  ln p = (d - log2 s1) ln 2 with d = fma(c, v, -ref) of a factor c
+rounded once: the rounding of c moves differences of z by 2^-24 of them, that of
+d the same; with Z the largest |z_v - z_max| asked for (and that of the values
+that make up s1, which is less), 3 Z 2^-24.  s1 adds positive terms, each with
+an exp2 of 2 units, one after another in at most V / 512 + 30 additions in a
+lane and 20 between lanes, waves and parts; log2 adds 2 units at |log2 s1| <=
+64.  So 2^-24 (3 Z + V / 512 + 200) in all.  The entropy is (log2 s1 - s2 / s1)
+ln 2 with s2's terms weighted by |d|: the same with (1 + ln V) for the terms'
+mean of |d| ln 2, which no distribution's exceeds by more than 2."""
+import math
+
+import pytest
+import torch
+
+import quant_ref as ref
+from paper_1808_00209_amd import bnn
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16, "int32": torch.int32}
+
+
+def _near(got, want, tol):
+    got, want = got.cpu().double(), want.double()
+    assert got.shape == want.shape
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got == -math.inf, want == -math.inf)
+    off = (got[fine] - want[fine]).abs()
+    assert not off.numel() or off.max() <= tol, (off.max(), tol)
+
+
+def _check(logits, ids=None, top_k=0, logit_scale=1.0, dev=None):
+    dev = logits.cuda() if dev is None else dev
+    got = bnn.bnn_logprobs(dev, None if ids is None else ids.cuda(), top_k, logit_scale)
+    torch.cuda.synchronize()
+    given, entropy, top_ids, top = ref.logprobs(logits, ids, top_k, logit_scale)
+    V = logits.shape[1]
+    Z = 0.0
+    for v in (given, top):
+        if v is not None and torch.isfinite(v).any():
+            Z = max(Z, -v[torch.isfinite(v)].min().item())
+    _near(got[1], entropy, 2.0 ** -24 * (V / 512 + 200) * (3 + math.log(V)))
+    tol = 2.0 ** -24 * (3 * Z + V / 512 + 200)
+    if ids is not None:
+        _near(got[0], given, tol)
+    else:
+        assert got[0] is None
+    if top_k:
+        assert torch.equal(got[2].cpu(), top_ids)
+        _near(got[3], top, tol)
+    else:
+        assert got[2] is None and got[3] is None
+
+
+def _logits(g, T, V, kind, spread=4.0):
+    z = spread * torch.randn(T, V, generator=g)
+    return (z * 16).round().to(torch.int32) if kind == "int32" else z.to(TYPES[kind])
+
+
+SIZES = [(1, 1), (2, 2), (1, 7), (5, 8), (3, 63), (300, 65), (4, 511), (7, 512), (2, 513), (1500, 1000), (5, 2047),
+         (3, 4096), (9, 4097), (1, 10000), (2, 32768), (1, 65536), (40, 5003), (3, 131072), (1100, 4500)]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("T, V", SIZES)
+def test_sizes(T, V, kind):
+    g = torch.Generator().manual_seed(31 * V + T)
+    scale = 1 / 16 if kind == "int32" else 1.0
+    for n, k in ((1, 1), (3, 8), (0, 0), (2, 32)):
+        ids = torch.randint(0, V, (T, n), generator=g, dtype=torch.int32) if n else None
+        _check(_logits(g, T, V, kind), ids[:, 0].contiguous() if n == 1 else ids, min(k, V), scale)
+
+
+@pytest.mark.parametrize("V", [100, 3000, 40000])
+@pytest.mark.parametrize("kind", ["fp32", "bf16", "fp16"])
+def test_answers_out_of_reach(V, kind):
+    """-inf at random, in all places but one, and everywhere."""
+    g = torch.Generator().manual_seed(V)
+    z = _logits(g, 12, V, kind)
+    z[0:3][torch.rand(3, V, generator=g) < 0.95] = -math.inf
+    z[3] = -math.inf
+    z[4] = -math.inf
+    z[4, V // 3] = -3.0
+    z[5, : V - 2] = -math.inf
+    z[6, 600:] = -math.inf
+    ids = torch.randint(-3, V + 3, (12, 40), generator=g, dtype=torch.int32)
+    ids[4, 0], ids[0, 0], ids[1, 0] = V // 3, -2 ** 31, 2 ** 31 - 1
+    _check(z, ids, 20)
+
+
+@pytest.mark.parametrize("V", [90, 5000, 70000])
+@pytest.mark.parametrize("kind", ["fp32", "bf16", "fp16"])
+def test_bad_rows(V, kind):
+    g = torch.Generator().manual_seed(V + 1)
+    z = _logits(g, 8, V, kind)
+    z[1, V // 2] = math.nan
+    z[2, V - 1] = math.inf
+    z[3, 0] = math.inf
+    z[3, 1:] = -math.inf
+    z[4] = math.nan
+    z[5, 3] = -math.nan
+    z[6, 5], z[6, V - 3] = math.inf, math.nan
+    ids = torch.randint(-1, V, (8, 9), generator=g, dtype=torch.int32)
+    _check(z, ids, 9)
+
+
+@pytest.mark.parametrize("V", [70, 3000, 50001])
+@pytest.mark.parametrize("kind", ["fp32", "bf16", "fp16"])
+def test_lowest_and_largest_values(V, kind):
+    """The type's lowest value is a value: a row of nothing else is uniform."""
+    g = torch.Generator().manual_seed(V + 2)
+    low, high = torch.finfo(TYPES[kind]).min, torch.finfo(TYPES[kind]).max
+    z = _logits(g, 9, V, kind)
+    z[0] = low
+    z[1, 5:] = low
+    z[2] = high
+    z[3] = 0
+    z[3, V - 1] = high
+    z[4] = -math.inf
+    z[4, V // 2:] = low
+    z[5, : V // 2], z[5, V // 2:] = low, high
+    z[6] = 0.0
+    z[6, ::2] = -0.0
+    z[7] += 100.0 if kind != "fp16" else 10.0
+    ids = torch.randint(0, V, (9, 3), generator=g, dtype=torch.int32)
+    for t, rows in (([0, 1, 2, 4, 5, 6, 7, 8], None), ([3], None)):
+        part, at = z[t].contiguous(), ids[t].contiguous()
+        dev = bnn.bnn_logprobs(part.cuda(), at.cuda(), 12)
+        given, entropy, top_ids, top = ref.logprobs(part, at, 12)
+        assert torch.equal(dev[2].cpu(), top_ids)
+        for a, b in ((dev[0], given), (dev[3], top)):
+            near = torch.isfinite(b) & (b.abs() < 1e4)
+            _near(a.cpu()[near], b[near], 2.0 ** -24 * (600 + V / 512))
+            far = torch.isfinite(b) & ~near  # (2^-22 of what lies outside fp32 may round to -inf)
+            got = a.cpu().double()[far]
+            assert ((got - b[far]).abs() <= 2.0 ** -22 * b[far].abs()).logical_or(
+                (got == -math.inf) & (b[far] < -3.4e38)).all()
+            assert torch.equal(torch.isnan(a.cpu()), torch.isnan(b))
+        _near(dev[1], entropy, 2.0 ** -24 * (V / 512 + 200) * (3 + math.log(V)))
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("V", [50, 1000, 4097, 40000])
+def test_orders(V, kind):
+    """Rising, falling, equal and few-valued rows: ties by the lowest index."""
+    g = torch.Generator().manual_seed(V + 3)
+    up = torch.arange(V).float() * (8.0 / V)
+    z = torch.stack([up, up.flip(0), torch.zeros(V), torch.randint(0, 3, (V,), generator=g).float(),
+                     (torch.arange(V) % 7).float(), (up * 4).floor(), -(up * 4).floor()])
+    scale = 1.0
+    if kind == "int32":
+        z, scale = (z * 64).round(), 1 / 64
+    z = z.to(TYPES[kind])
+    ids = torch.randint(0, V, (7, 2), generator=g, dtype=torch.int32)
+    for k in (1, 5, 32):
+        _check(z, ids, k, scale)
+
+
+@pytest.mark.parametrize("V", [60, 9000])
+def test_int32_extremes(V):
+    """Sums beyond 2^24, which fp32 would not tell apart: their order is theirs."""
+    z = torch.full((4, V), -2 ** 31, dtype=torch.int32)
+    z[0, 3], z[0, 4], z[0, 5] = 2 ** 24 + 1, 2 ** 24, 2 ** 24 + 2
+    z[1] = 2 ** 31 - 1
+    z[2] = torch.arange(V, dtype=torch.int32) + 2 ** 30
+    ids = torch.tensor([[3], [0], [V - 1], [1]], dtype=torch.int32)
+    _check(z, ids, 6, 2.0 ** -40)
+
+
+def test_strides_and_temperature():
+    g = torch.Generator().manual_seed(12)
+    for kind in TYPES:
+        for V, stride, first in ((33, 40, 1), (5001, 5003, 3), (1000, 1001, 0)):
+            flat = _logits(g, 1, first + 9 * stride, kind)[0]
+            z = flat[first:].as_strided((9, V), (stride, 1))
+            dev = flat.cuda()[first:].as_strided((9, V), (stride, 1))
+            ids = torch.randint(0, V, (9, 2), generator=g, dtype=torch.int32)
+            for scale in (0.05, 2.5):
+                _check(z, ids, 10, scale, dev=dev)
+
+
+def test_caller_s_outputs_and_workspace():
+    """A workspace of many rows serves any fewer; outputs of the caller's."""
+    g = torch.Generator().manual_seed(13)
+    V = 20000
+    bytes_ = [bnn.bnn_logprobs_workspace_size(bnn.LogprobsDesc(T, V, 0, 8, 0, 1.0)) for T in
+              (1, 2, 50, 300, 1023, 1024, 5000)]
+    assert bytes_ == sorted(bytes_)
+    ws = torch.empty(bytes_[-1], dtype=torch.uint8, device="cuda")
+    for T in (1, 2, 50, 1030):
+        z = _logits(g, T, V, "bf16")
+        ids = torch.randint(0, V, (T,), generator=g, dtype=torch.int32)
+        lp, en = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+        ti, tl = torch.empty(T, 8, device="cuda", dtype=torch.int32), torch.empty(T, 8, device="cuda")
+        got = bnn.bnn_logprobs(z.cuda(), ids.cuda(), 8, logp=lp, entropy=en, top_ids=ti, top_logp=tl, workspace=ws)
+        assert got[0] is lp and got[1] is en and got[2] is ti and got[3] is tl
+        again = bnn.bnn_logprobs(z.cuda(), ids.cuda(), 8)
+        assert all(torch.equal(a, b) for a, b in zip(got, again))
+    only = bnn.bnn_logprobs(z.cuda(), None, 3, want_entropy=False)
+    assert only[0] is None and only[1] is None and torch.equal(only[2], ti[:, :3])
+    none = bnn.bnn_logprobs(z.cuda()[:0], ids.cuda()[:0], 3)
+    assert none[0].shape == (0,) and none[2].shape == (0, 3)
+
+
+def test_far_rows():
+    """Rows beyond 4 GiB from the first."""
+    V, stride = 3000, 3 << 29
+    flat = torch.zeros(2 * stride + V, dtype=torch.bfloat16, device="cuda")
+    z = flat.as_strided((3, V), (stride, 1))
+    g = torch.Generator().manual_seed(14)
+    host = _logits(g, 3, V, "bf16")
+    z.copy_(host)
+    _check(host, torch.tensor([1, 2999, 5], dtype=torch.int32), 5, dev=z)
