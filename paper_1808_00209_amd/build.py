@@ -25,7 +25,7 @@ SOURCES = ["pack.hip", "bconv_valu.hip", "bconv_mfma.hip", "bconv_tile.hip", "bc
            "experts.hip", "experts_tile.hip", "experts_skinny.hip",
            "experts_combine.hip", "experts_sum_rows.hip",
            "lora.hip", "lora_tile.hip", "lora_skinny.hip", "rmsnorm.hip", "q8gemm.hip",
-           "q8gemm_skinny.hip", "logprobs.hip",
+           "q8gemm_skinny.hip", "q8gemm_tile.hip", "logprobs.hip",
            "api.cpp", "experts_api.cpp", "quant_api.cpp"]
 ARCH = os.environ.get("BNN_OFFLOAD_ARCH", "gfx950")
 

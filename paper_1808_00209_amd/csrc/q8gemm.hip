@@ -33,7 +33,7 @@ __device__ __forceinline__ v4i load16(const int8_t* row, int k, int K) {
 
 // A workgroup of 2 x 2 waves, 64 TM rows x 64 TN outputs.
 template <class T, int TM, int TN>
-__global__ __launch_bounds__(kNT) void q8_tile_kernel(Q8Args a) {
+__global__ __launch_bounds__(kNT) void q8_any_kernel(Q8Args a) {
   extern __shared__ v4i lds[];
   constexpr int BM = 64 * TM, BN = 64 * TN;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -98,13 +98,18 @@ __global__ __launch_bounds__(kNT) void q8_tile_kernel(Q8Args a) {
 }  // namespace
 
 hipError_t launch_q8gemm(const Q8Args& a, hipStream_t s) {
-  if (q8_skinny_takes(a)) return launch_q8_skinny(a, s);
+  auto on16 = [](const void* p, int64_t stride) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0;
+  };
+  const Q8Form form = q8_form(a.M, a.N, a.K, on16(a.x, a.x_stride) && on16(a.w, a.w_stride));
+  if (form == kQ8Skinny) return launch_q8_skinny(a, s);
+  if (form != kQ8Any) return launch_q8_tile(a, form, s);
   constexpr int TM = 2, TN = 2;
   const int64_t cols = (a.N + 64 * TN - 1) / (64 * TN), rows = (a.M + 64 * TM - 1) / (64 * TM);
   const unsigned grid = static_cast<unsigned>(rows * cols);  // M * N <= 2^35: below 2^23 + 2^18
   with_real_type(a.dtype, [&](auto t) {
     using T = decltype(t);
-    q8_tile_kernel<T, TM, TN><<<grid, kNT, size_t{64} * (TM + TN) * kBK, s>>>(a);
+    q8_any_kernel<T, TM, TN><<<grid, kNT, size_t{64} * (TM + TN) * kBK, s>>>(a);
   });
   return hipGetLastError();
 }

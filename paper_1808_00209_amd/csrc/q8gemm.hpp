@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "dtypes.hpp"
+#include "q8_plans.hpp"
 #include "quant.hpp"
 
 namespace bnn {
@@ -31,7 +32,9 @@ __device__ __forceinline__ T q8_output(int32_t sum, float xs, float ws, float bi
 }
 
 // Few rows: every weight read once (q8gemm_skinny.hip).
-bool q8_skinny_takes(const Q8Args& a);
 hipError_t launch_q8_skinny(const Q8Args& a, hipStream_t s);
+
+// Many rows on 16-byte steps (q8gemm_tile.hip): one of the tile forms.
+hipError_t launch_q8_tile(const Q8Args& a, Q8Form form, hipStream_t s);
 
 }  // namespace bnn

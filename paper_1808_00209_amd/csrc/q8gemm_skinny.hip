@@ -108,10 +108,6 @@ __global__ __launch_bounds__(kNT) void q8_skinny_kernel(Q8Args a, int kw_log, in
 
 }  // namespace
 
-bool q8_skinny_takes(const Q8Args& a) {
-  return a.K >= 16 && a.K <= 8 * kWaves * kStep * 2 && a.M <= 64 && (a.M <= 32 || a.K <= 4096);
-}
-
 hipError_t launch_q8_skinny(const Q8Args& a, hipStream_t s) {
   const int all = (a.K + kStep - 1) / kStep;  // steps of a row
   const int kw_log = all >= 16 ? 3 : all >= 8 ? 2 : all >= 4 ? 1 : 0;

@@ -49,7 +49,12 @@ SIZES = [(1, 1, 1), (1, 5, 3), (1, 16, 64), (1, 33, 100), (1, 4096, 4096), (1, 1
          (3, 257, 129), (7, 2050, 1100), (8, 4096, 512), (16, 100, 8192), (17, 300, 700), (31, 64, 4096),
          (32, 1024, 1024), (33, 65, 4111), (63, 129, 255), (64, 512, 640), (65, 64, 127), (100, 100, 128),
          (128, 128, 256), (129, 257, 130), (200, 1030, 2050), (256, 4096, 4096), (777, 2050, 1100),
-         (513, 511, 1029), (1024, 1024, 1024), (2050, 300, 96), (300, 4100, 17), (1500, 1500, 512)]
+         (513, 511, 1029), (1024, 1024, 1024), (2050, 300, 96), (300, 4100, 17), (1500, 1500, 512),
+         # tiles of 128 (one and two per CU) and 256, K shorter than a stage, of
+         # whole stages, and short last ones with whole chunks and without
+         (1000, 4100, 100), (2000, 2000, 16), (1100, 3900, 1024), (1030, 3700, 1104), (2000, 4200, 31),
+         (2000, 4100, 384), (2100, 4000, 400), (4100, 3900, 16), (3900, 4100, 256), (3850, 4000, 1029),
+         (4096, 4096, 640), (4000, 4001, 99)]
 
 
 @pytest.mark.parametrize("M, N, K", SIZES)
