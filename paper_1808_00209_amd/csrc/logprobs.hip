@@ -16,14 +16,16 @@
 // largest values reach.
 #include "dtypes.hpp"
 #include "quant.hpp"
+#include "wave_ops.hpp"
 
 #include <type_traits>
 
 namespace bnn {
 namespace {
 
-constexpr int kNT = 256;
-constexpr int kGroup = 512;   // values of a wave's step: 8 per lane
+constexpr int kNT = 256;  // unless a row has more waves
+constexpr int kEach = 16;           // values of a lane per step, in groups of 8
+constexpr int kStep = 64 * kEach;   // of a wave
 constexpr float kAway = 60.0f;
 constexpr float kFar = 3e38f;
 
@@ -79,19 +81,8 @@ __device__ __forceinline__ Eight<T> load8(const T* p) {
   return e;
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
-  return v;
-}
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) v = __builtin_fmaxf(v, __shfl_xor(v, o));
-  return v;
-}
-
-// A wave's sorted list of keys, the largest in lane 0; bound is the key of lane
-// top_k - 1 (0: the list is not full), floor what a value's order must reach.
+// A wave's sorted list of keys over its lanes, the largest in lane 0 (0: none).
+// bound is the key of lane top_k - 1, floor what a value's order must reach.
 struct Top {
   uint32_t hi, lo;  // this lane's key
   uint32_t floor;   // uniform
@@ -99,9 +90,9 @@ struct Top {
 
   __device__ __forceinline__ void insert(uint64_t key, int top_k) {
     const uint64_t mine = static_cast<uint64_t>(hi) << 32 | lo;
-    const int pos = __popcll(__ballot(mine > key));
+    const int pos = __popcll(__ballot(mine > key));  // (below top_k: key > bound)
     const int lane = threadIdx.x & 63;
-    const uint32_t uh = __shfl_up(hi, 1), ul = __shfl_up(lo, 1);
+    const uint32_t uh = lane_before(hi), ul = lane_before(lo);
     hi = lane < pos ? hi : lane == pos ? static_cast<uint32_t>(key >> 32) : uh;
     lo = lane < pos ? lo : lane == pos ? static_cast<uint32_t>(key) : ul;
     const uint32_t bh = __builtin_amdgcn_readlane(hi, top_k - 1);
@@ -111,12 +102,15 @@ struct Top {
   }
 };
 
-// Raises top.floor to an order that the values of at least top_k lanes reach, if
-// there is a higher one (to 16 bits: a lower bound is all it is).
+// Raises top.floor to an order that the values of at least top_k lanes reach
+// (mine: a lane's largest, 0 for none): ten bits of it below those that all
+// lanes' have in common, a lower bound of the top_k-th being all that is asked.
 __device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) {
-  uint32_t at = 0;
-#pragma unroll
-  for (int b = 31; b >= 16; --b) {
+  const uint32_t most = wave_max(mine), least = wave_min(mine ? mine : ~0u);
+  const int own = most == least ? 0 : 32 - __builtin_clz(most ^ least);  // bits
+  uint32_t at = own < 32 ? most >> own << own : 0;
+  if (__popcll(__ballot(mine >= at && mine != 0)) < top_k) return;
+  for (int b = own - 1; b >= 0 && b >= own - 10; --b) {
     const uint32_t next = at | 1u << b;
     if (__popcll(__ballot(mine >= next)) >= top_k) at = next;
   }
@@ -139,7 +133,9 @@ struct Scan {
     if constexpr (SAFE) return v == -__builtin_inff() ? v : (v - ref) * c;
     else return __builtin_fmaf(v, c, -ref);
   }
-  __device__ __forceinline__ void add(const float (&v)[8], float fm) {
+  // FINITE: no value is -inf.
+  template <bool FINITE>
+  __device__ __forceinline__ void add(const float (&v)[kEach], float fm) {
     if (__any(SAFE ? fm > ref : delta(fm) > kAway)) {
       const float top = wave_max(fm);
       const float next = SAFE ? top : __builtin_fminf(__builtin_fmaxf(top * c, -kFar), kFar);
@@ -150,18 +146,21 @@ struct Scan {
       s1 *= f;
       ref = next;
     }
-    float e[8], d[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      d[i] = delta(v[i]);
-      e[i] = exp2_of(d[i]);
-      d[i] = __builtin_fmaxf(d[i], -200.0f);  // (0 * -inf)
+    for (int g = 0; g < kEach; g += 8) {
+      float e[8], d[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[i] = delta(v[g + i]);
+        e[i] = exp2_of(d[i]);
+        if (!FINITE) d[i] = __builtin_fmaxf(d[i], -200.0f);  // (0 * -inf)
+      }
+      s1 += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      float t = e[0] * d[0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) t = __builtin_fmaf(e[i], d[i], t);
+      s2 += t;
     }
-    s1 += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-    float t = e[0] * d[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) t = __builtin_fmaf(e[i], d[i], t);
-    s2 += t;
   }
   __device__ __forceinline__ Sums total() const {
     return {SAFE ? static_cast<double>(ref) * c : static_cast<double>(ref), wave_sum(s1),
@@ -187,63 +186,92 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
                                      float c, int top_k, Top& top) {
   using R = typename RawOf<T>::type;
   constexpr bool kInts = std::is_same<R, int32_t>::value;
+  constexpr int kGroups = kEach / 8;
   const int lane = threadIdx.x & 63;
   Scan<SAFE> sc;
   sc.start(c);
-  // 8 values per lane from index `at` on, the lane's first n of them in the row.
-  auto step = [&](const R (&v)[8], int at, int n, auto part) {
-    constexpr bool kPart = decltype(part)::value;
-    float f[8];
+  // A step: group g of a lane's 8 values starts at index at + 512 g + 8 lane.
+  // What lies past the row's end is -inf; integers have no such value, so there
+  // `n` says how many of each group are in the row (part: of some lane, not 8).
+  auto step = [&](const R (&v)[kEach], int at, const int (&n)[kGroups], auto part) {
+    constexpr bool kPart = kInts && decltype(part)::value;
+    float f[kEach];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      f[i] = !kPart || i < n ? static_cast<float>(v[i]) : -__builtin_inff();
-    float most = f[0];
+    for (int i = 0; i < kEach; ++i) {
+      f[i] = static_cast<float>(v[i]);
+      if (kPart) f[i] = i % 8 < n[i / 8] ? f[i] : -__builtin_inff();
+    }
+    R m = v[0];
+    if constexpr (kInts) {  // (beyond 2^24 their order is not that of f)
 #pragma unroll
-    for (int i = 1; i < 8; ++i) most = __builtin_fmaxf(most, f[i]);
-    sc.add(f, most);
+      for (int i = 1; i < kEach; ++i) m = m > v[i] ? m : v[i];
+    } else {
+#pragma unroll
+      for (int i = 1; i < kEach; ++i) m = __builtin_fmaxf(m, v[i]);
+    }
+    const bool some = !kPart || n[0] > 0;  // (past the end: the least integer)
+    sc.template add<kInts && !kPart>(f, some ? static_cast<float>(m) : -__builtin_inff());
     if constexpr (TOP) {
-      uint32_t mo;
-      if constexpr (kInts) {  // (beyond 2^24 their order is not that of f)
-        R m = v[0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i)
-          if (!kPart || i < n) m = m > v[i] ? m : v[i];
-        mo = kPart && n <= 0 ? 0u : order_of(m);
-      } else {
-        mo = order_of(most);
-      }
-      const uint64_t reach = __ballot(mo >= top.floor);
+      const uint32_t mo = some ? order_of(m) : 0u;
+      const uint64_t reach = __ballot(some && mo >= top.floor);
       if (reach) {
         if (__popcll(reach) > 12) raise_floor(top, mo, top_k);
+        R floor;
+        value_of(top.floor, floor);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t o = order_of(v[i]);
-          uint64_t mask = __ballot(o >= top.floor && (!kPart || i < n));
+        for (int i = 0; i < kEach; ++i) {
+          uint64_t mask = __ballot(v[i] >= floor && (!kPart || i % 8 < n[i / 8]));
           while (mask) {
             const int l = __builtin_ctzll(mask);
             mask &= mask - 1;
-            const uint32_t oh = __builtin_amdgcn_readlane(o, l);
-            const uint32_t index = static_cast<uint32_t>(at + 8 * l + i);
-            const uint64_t key = static_cast<uint64_t>(oh) << 32 | static_cast<uint32_t>(~index);
-            if (key > top.bound) top.insert(key, top_k);
+            const uint32_t o = order_of(__builtin_bit_cast(
+                R, __builtin_amdgcn_readlane(__builtin_bit_cast(uint32_t, v[i]), l)));
+            const uint32_t index = static_cast<uint32_t>(at + i / 8 * 512 + 8 * l + i % 8);
+            const uint64_t key = static_cast<uint64_t>(o) << 32 | static_cast<uint32_t>(~index);
+            if (key > top.bound) {
+              top.insert(key, top_k);
+              value_of(top.floor, floor);
+            }
           }
         }
       }
     }
   };
-  for (int at = begin + wave * kGroup; at < end; at += waves * kGroup) {
-    const int i0 = at + 8 * lane;
-    R v[8];
-    if (at + kGroup <= end) {
-      const Eight<T> e = load8(row + i0);
+  T past;
+  if constexpr (kInts) past = INT32_MIN;
+  else past = static_cast<T>(-__builtin_inff());
+  R v[kEach];
+  int n[kGroups] = {};
+  auto take = [&](const Eight<T> (&e)[kGroups]) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = static_cast<R>(e.v[i]);
-      step(v, at, 8, std::false_type{});
-    } else {
+    for (int i = 0; i < kEach; ++i) v[i] = static_cast<R>(e[i / 8].v[i % 8]);
+  };
+  int at = begin + wave * kStep;
+  for (; at + kStep <= end; at += waves * kStep) {
+    Eight<T> e[kGroups];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i0 + i < end ? static_cast<R>(row[i0 + i]) : R(0);
-      step(v, at, end - i0, std::true_type{});
+    for (int g = 0; g < kGroups; ++g) e[g] = load8(row + at + 512 * g + 8 * lane);
+    take(e);
+    step(v, at, n, std::false_type{});
+  }
+  if (at < end) {
+    Eight<T> e[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int first = at + 512 * g + 8 * lane;
+      n[g] = end - first;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[g].v[i] = past;
+      if (n[g] >= 8) {
+        e[g] = load8(row + first);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+          if (i < n[g]) e[g].v[i] = row[first + i];
+      }
     }
+    take(e);
+    step(v, at, n, std::true_type{});
   }
   return sc.total();
 }
@@ -258,6 +286,47 @@ __device__ __forceinline__ Sums wave_part(const T* row, int begin, int end, int 
   return s;
 }
 
+// The top_k largest of `count` keys in lists of top_k, `stride` apart (0: none),
+// by one wave.
+__device__ __forceinline__ Top select_keys(const uint64_t* keys, int count, int stride, int top_k) {
+  const int lane = threadIdx.x & 63;
+  auto at = [&](int i) {
+    const int list = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(top_k));
+    return i < count ? keys[list * stride + i - list * top_k] : uint64_t{0};
+  };
+  Top top = {0, 0, 0, 0};
+  uint32_t most = 0;
+  for (int i = lane; i < count; i += 64) {
+    const uint32_t o = static_cast<uint32_t>(at(i) >> 32);
+    most = most > o ? most : o;
+  }
+  raise_floor(top, most, top_k);
+  for (int i0 = 0; i0 < count; i0 += 64) {
+    const uint64_t key = at(i0 + lane);
+    const uint32_t hi = static_cast<uint32_t>(key >> 32), lo = static_cast<uint32_t>(key);
+    uint64_t mask = __ballot(hi >= top.floor && key > top.bound);
+    while (mask) {
+      const int l = __builtin_ctzll(mask);
+      mask &= mask - 1;
+      const uint64_t k = static_cast<uint64_t>(__builtin_amdgcn_readlane(hi, l)) << 32 |
+                         static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, l));
+      if (k > top.bound) top.insert(k, top_k);
+    }
+  }
+  return top;
+}
+
+// Sums over the wave's lanes.
+__device__ __forceinline__ Sums lanes_joined(Sums s) {
+  const double ref = wave_max(s.s1 == 0.0f ? -__builtin_inf() : s.ref);
+  if (s.s1 == 0.0f) s.ref = ref;
+  // (a part with NaN for sums: NaN, whatever its reference)
+  const float move = ref > -__builtin_inf() ? fmaxf(static_cast<float>(s.ref - ref), -1e4f) : 0.0f;
+  const float f = exp2_of(move);
+  return {ref > -__builtin_inf() ? ref : 0.0, wave_sum(f * s.s1),
+          wave_sum(f * __builtin_fmaf(move, s.s1, s.s2))};
+}
+
 // A row's outputs from its sums and (lane j: the j-th) keys, by one wave.
 template <class T>
 __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t t, const Sums& s,
@@ -266,16 +335,21 @@ __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t t, cons
   constexpr double kLn2 = 0.693147180559945309417;
   const int lane = threadIdx.x & 63;
   const bool none = s.s1 == 0.0f, bad = !(s.s1 < __builtin_inff());
-  const float ls = log2f(s.s1);
+  // (2^-60 <= s1 < 2^24 2^60, or 1 <= s1 <= 2^24 by the safe form)
+  const float ls = __builtin_amdgcn_logf(s.s1);
+  const bool small = __builtin_fabs(s.ref) < 1e30;
+  const float ref = static_cast<float>(s.ref);
   const float nan = __builtin_nanf("");
   auto ln_p = [&](R v) {
     if (std::is_same<R, float>::value && static_cast<float>(v) == -__builtin_inff())
       return -__builtin_inff();
+    const float d = __builtin_fmaf(static_cast<float>(v), c, -ref);
+    if (small && __builtin_fabsf(d) < 1e30f) return (d - ls) * static_cast<float>(kLn2);
     return static_cast<float>((static_cast<double>(v) * c - s.ref - static_cast<double>(ls)) * kLn2);
   };
   if (a.entropy && lane == 0)
     a.entropy[t] = bad ? nan : none ? 0.0f
-        : static_cast<float>(static_cast<double>(ls - s.s2 / s.s1) * kLn2);
+        : (ls - s.s2 / s.s1) * static_cast<float>(kLn2);
   for (int j = lane; j < a.n; j += 64) {
     const int id = a.ids[t * a.n + j];
     float lp = -__builtin_inff();
@@ -301,18 +375,19 @@ __device__ __forceinline__ float factor_of(float scale) {
 
 // W waves per part of a row: whole rows (splits 1), or parts to the workspace.
 template <class T, int W, bool TOP>
-__global__ __launch_bounds__(kNT) void logprobs_kernel(LogprobsArgs a, int splits, int length) {
+__global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(LogprobsArgs a, int splits,
+                                                                        int length) {
   using R = typename RawOf<T>::type;
   __shared__ Sums sums[W];
   __shared__ uint64_t keys[W][BNN_MAX_ALTERNATIVES];
-  constexpr int kParts = kNT / 64 / W;  // of a workgroup
+  constexpr int kParts = W > 4 ? 1 : 4 / W;  // of a workgroup
   const int lane = threadIdx.x & 63;
-  const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t part = static_cast<int64_t>(blockIdx.x) * kParts +
-                       (W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
-  const int64_t t = part / splits;
+  const int id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = W == 1 ? 0 : id;
+  const int64_t part = static_cast<int64_t>(blockIdx.x) * kParts + (W == 1 ? id : 0);
+  // (split rows: T < kFull, so that parts fit 32 bits)
+  const int64_t t = splits == 1 ? part : static_cast<uint32_t>(part) / static_cast<uint32_t>(splits);
   if (t >= a.T) return;
-  const int begin = static_cast<int>(part % splits) * length;
+  const int begin = static_cast<int>(part - t * splits) * length;
   const int end = min(begin + length, a.V);
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
   const float c = factor_of(a.scale);
@@ -320,21 +395,12 @@ __global__ __launch_bounds__(kNT) void logprobs_kernel(LogprobsArgs a, int split
   Sums s = wave_part<T, TOP>(row, begin, end, wave, W, c, a.top_k, top);
   if constexpr (W > 1) {
     if (lane == 0) sums[wave] = s;
-    if (TOP && lane < a.top_k)
-      keys[wave][lane] = static_cast<uint64_t>(top.hi) << 32 | top.lo;
+    if (TOP && lane < a.top_k) keys[wave][lane] = static_cast<uint64_t>(top.hi) << 32 | top.lo;
     __syncthreads();
     if (wave != 0) return;
-#pragma unroll 1
-    for (int w = 1; w < W; ++w) {
-      s = joined(s, sums[w]);
-      if constexpr (TOP) {
-        for (int j = 0; j < a.top_k; ++j) {
-          const uint64_t key = keys[w][j];
-          if (!(key > top.bound)) break;
-          top.insert(key, a.top_k);
-        }
-      }
-    }
+    s = lane < W ? sums[lane < W ? lane : 0] : Sums{0.0, 0.0f, 0.0f};
+    s = lanes_joined(s);
+    if constexpr (TOP) top = select_keys(&keys[0][0], W * a.top_k, BNN_MAX_ALTERNATIVES, a.top_k);
   }
   const uint64_t key = static_cast<uint64_t>(top.hi) << 32 | top.lo;
   if (splits == 1) {
@@ -350,35 +416,38 @@ __global__ __launch_bounds__(kNT) void logprobs_kernel(LogprobsArgs a, int split
 template <class T>
 __global__ __launch_bounds__(64) void join_kernel(LogprobsArgs a, int splits) {
   const int64_t t = blockIdx.x;
-  const int lane = threadIdx.x;
-  const char* at = static_cast<const char*>(a.workspace) + t * splits * part_bytes(a.top_k);
+  const int bytes = static_cast<int>(part_bytes(a.top_k));
+  const char* at = static_cast<const char*>(a.workspace) + t * splits * bytes;
   Sums s = {0.0, 0.0f, 0.0f};
-  Top top = {0, 0, 0, 0};
-  for (int p = 0; p < splits; ++p) {
-    const char* part = at + p * part_bytes(a.top_k);
-    s = joined(s, reinterpret_cast<const Part*>(part)->sums);
-    for (int j = 0; j < a.top_k; ++j) {
-      const uint64_t key = reinterpret_cast<const uint64_t*>(part + sizeof(Part))[j];
-      if (!(key > top.bound)) break;
-      top.insert(key, a.top_k);
-    }
+  for (int p0 = 0; p0 < splits; p0 += 64) {
+    const int p = p0 + static_cast<int>(threadIdx.x);
+    Sums more = {0.0, 0.0f, 0.0f};
+    if (p < splits) more = reinterpret_cast<const Part*>(at + p * bytes)->sums;
+    more = lanes_joined(more);
+    s = p0 == 0 ? more : joined(s, more);
   }
-  (void)lane;
+  Top top = {0, 0, 0, 0};
+  if (a.top_k > 0)
+    top = select_keys(reinterpret_cast<const uint64_t*>(at + sizeof(Part)), splits * a.top_k, bytes / 8,
+                      a.top_k);
   write_row<T>(a, t, s, static_cast<uint64_t>(top.hi) << 32 | top.lo, factor_of(a.scale));
 }
 
-constexpr int kParts = 1024;     // parts that fill the card
-constexpr int kLength = 2048;    // a part's values, at least
+// Rows that fill the card with a workgroup each; fewer are split.
+constexpr int kFull = 256;
+constexpr int kParts = 1024;       // parts that fill it
+constexpr int kLength = 4 * kStep; // a part's values, at least
 
 int64_t most_splits(int32_t V) { return (V + kLength - 1) / kLength; }
 int64_t splits_of(int64_t T, int32_t V) {
+  if (T >= kFull) return 1;
   const int64_t want = (kParts + T - 1) / T;
   return want < most_splits(V) ? want : most_splits(V);
 }
 
 }  // namespace
 
-// (Rows times splits never pass kParts + T - 1 with T < kParts, nor T times the
+// (Rows times splits never pass kParts + T - 1 with T < kFull, nor T times the
 // most splits: a bound that does not fall as T grows.)
 size_t logprobs_workspace(int64_t T, int32_t V, int32_t top_k) {
   if (most_splits(V) < 2) return 0;
@@ -388,18 +457,19 @@ size_t logprobs_workspace(int64_t T, int32_t V, int32_t top_k) {
 
 hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t s) {
   const int splits = static_cast<int>(splits_of(a.T, a.V));
-  const int length = ((a.V + splits - 1) / splits + kGroup - 1) / kGroup * kGroup;
+  const int length = ((a.V + splits - 1) / splits + kStep - 1) / kStep * kStep;
   auto go = [&](auto t) {
     using T = decltype(t);
     auto with = [&](auto wc, auto tc) {
       constexpr int W = decltype(wc)::value;
-      constexpr int per = kNT / 64 / W;
+      constexpr int per = W > 4 ? 1 : 4 / W;
       const int64_t parts = a.T * splits;
       logprobs_kernel<T, W, decltype(tc)::value>
-          <<<static_cast<unsigned>((parts + per - 1) / per), kNT, 0, s>>>(a, splits, length);
+          <<<static_cast<unsigned>((parts + per - 1) / per), W > 4 ? W * 64 : kNT, 0, s>>>(a, splits, length);
     };
     auto waves = [&](auto tc) {
       if (a.V <= 4096) with(std::integral_constant<int, 1>{}, tc);
+      else if (splits == 1 && a.T < 2 * kParts && a.V >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
       else with(std::integral_constant<int, 4>{}, tc);
     };
     if (a.top_k > 0) waves(std::true_type{});
