@@ -87,6 +87,47 @@ struct Top {
   uint32_t hi, lo;  // this lane's key
   uint32_t floor;   // uniform
   uint64_t bound;   // uniform
+  uint64_t* slots;  // 64 of the wave's, in LDS
+
+  __device__ __forceinline__ void take_bound(int top_k) {
+    const uint32_t bh = __builtin_amdgcn_readlane(hi, top_k - 1);
+    bound = static_cast<uint64_t>(bh) << 32 |
+            static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, top_k - 1));
+    if (bh > floor) floor = bh;
+  }
+
+  // A key of the lanes where `is` holds, put behind the `count` ones in slots
+  // (past 64: only counted).
+  __device__ __forceinline__ void collect(uint64_t key, bool is, int& count) {
+    const uint64_t mask = __ballot(is);
+    if (!mask) return;
+    const int at = count + __builtin_amdgcn_mbcnt_hi(
+        static_cast<uint32_t>(mask >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0));
+    if (is && at < 64) slots[at] = key;
+    count += __popcll(mask);
+  }
+
+  // An empty list from the `count` <= 64 keys in slots: a key's place is the
+  // number of larger ones, counted over all of them with nothing to wait for.
+  __device__ __forceinline__ void fill(int count, int top_k) {
+    const int lane = threadIdx.x & 63;
+    const uint64_t mine = lane < count ? slots[lane] : 0;
+    const uint32_t mh = static_cast<uint32_t>(mine >> 32), ml = static_cast<uint32_t>(mine);
+    int place = 0;
+    for (int j = 0; j < count; j += 4) {  // (keys past count are 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t other = static_cast<uint64_t>(__builtin_amdgcn_readlane(mh, j + i)) << 32 |
+                               static_cast<uint32_t>(__builtin_amdgcn_readlane(ml, j + i));
+        place += other > mine;
+      }
+    }
+    if (lane < count) slots[place] = mine;
+    const uint64_t key = lane < top_k && lane < count ? slots[lane] : 0;
+    hi = static_cast<uint32_t>(key >> 32);
+    lo = static_cast<uint32_t>(key);
+    take_bound(top_k);
+  }
 
   __device__ __forceinline__ void insert(uint64_t key, int top_k) {
     const uint64_t mine = static_cast<uint64_t>(hi) << 32 | lo;
@@ -95,10 +136,7 @@ struct Top {
     const uint32_t uh = lane_before(hi), ul = lane_before(lo);
     hi = lane < pos ? hi : lane == pos ? static_cast<uint32_t>(key >> 32) : uh;
     lo = lane < pos ? lo : lane == pos ? static_cast<uint32_t>(key) : ul;
-    const uint32_t bh = __builtin_amdgcn_readlane(hi, top_k - 1);
-    bound = static_cast<uint64_t>(bh) << 32 |
-            static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, top_k - 1));
-    if (bh > floor) floor = bh;
+    take_bound(top_k);
   }
 };
 
@@ -218,16 +256,31 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
         if (__popcll(reach) > 12) raise_floor(top, mo, top_k);
         R floor;
         value_of(top.floor, floor);
+        auto passes = [&](int i) { return v[i] >= floor && (!kPart || i % 8 < n[i / 8]); };
+        auto index_of = [&](int i, int l) { return static_cast<uint32_t>(at + i / 8 * 512 + 8 * l + i % 8); };
+        if (top.bound == 0) {  // (the list is not full: most often, empty)
+          const bool empty = __builtin_amdgcn_readlane(top.hi | top.lo, 0) == 0;
+          int count = 0;
+          if (empty) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+              top.collect(static_cast<uint64_t>(order_of(v[i])) << 32 | static_cast<uint32_t>(~index_of(i, lane)),
+                          passes(i), count);
+          }
+          if (empty && count <= 64) {
+            top.fill(count, top_k);
+            return;
+          }
+        }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-          uint64_t mask = __ballot(v[i] >= floor && (!kPart || i % 8 < n[i / 8]));
+          uint64_t mask = __ballot(passes(i));
           while (mask) {
             const int l = __builtin_ctzll(mask);
             mask &= mask - 1;
             const uint32_t o = order_of(__builtin_bit_cast(
                 R, __builtin_amdgcn_readlane(__builtin_bit_cast(uint32_t, v[i]), l)));
-            const uint32_t index = static_cast<uint32_t>(at + i / 8 * 512 + 8 * l + i % 8);
-            const uint64_t key = static_cast<uint64_t>(o) << 32 | static_cast<uint32_t>(~index);
+            const uint64_t key = static_cast<uint64_t>(o) << 32 | static_cast<uint32_t>(~index_of(i, l));
             if (key > top.bound) {
               top.insert(key, top_k);
               value_of(top.floor, floor);
@@ -288,19 +341,29 @@ __device__ __forceinline__ Sums wave_part(const T* row, int begin, int end, int 
 
 // The top_k largest of `count` keys in lists of top_k, `stride` apart (0: none),
 // by one wave.
-__device__ __forceinline__ Top select_keys(const uint64_t* keys, int count, int stride, int top_k) {
+__device__ __forceinline__ Top select_keys(const uint64_t* keys, int count, int stride, int top_k,
+                                           uint64_t* slots) {
   const int lane = threadIdx.x & 63;
   auto at = [&](int i) {
     const int list = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(top_k));
     return i < count ? keys[list * stride + i - list * top_k] : uint64_t{0};
   };
-  Top top = {0, 0, 0, 0};
+  Top top = {0, 0, 0, 0, slots};
   uint32_t most = 0;
   for (int i = lane; i < count; i += 64) {
     const uint32_t o = static_cast<uint32_t>(at(i) >> 32);
     most = most > o ? most : o;
   }
   raise_floor(top, most, top_k);
+  int collected = 0;
+  for (int i0 = 0; i0 < count; i0 += 64) {
+    const uint64_t key = at(i0 + lane);
+    top.collect(key, key != 0 && static_cast<uint32_t>(key >> 32) >= top.floor, collected);
+  }
+  if (collected <= 64) {
+    top.fill(collected, top_k);
+    return top;
+  }
   for (int i0 = 0; i0 < count; i0 += 64) {
     const uint64_t key = at(i0 + lane);
     const uint32_t hi = static_cast<uint32_t>(key >> 32), lo = static_cast<uint32_t>(key);
@@ -380,6 +443,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(Logprobs
   using R = typename RawOf<T>::type;
   __shared__ Sums sums[W];
   __shared__ uint64_t keys[W][BNN_MAX_ALTERNATIVES];
+  __shared__ uint64_t slots[W > 4 ? W : 4][64];
   constexpr int kParts = W > 4 ? 1 : 4 / W;  // of a workgroup
   const int lane = threadIdx.x & 63;
   const int id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = W == 1 ? 0 : id;
@@ -391,7 +455,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(Logprobs
   const int end = min(begin + length, a.V);
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
   const float c = factor_of(a.scale);
-  Top top = {0, 0, kFloor<R>, 0};
+  Top top = {0, 0, kFloor<R>, 0, slots[id]};
   Sums s = wave_part<T, TOP>(row, begin, end, wave, W, c, a.top_k, top);
   if constexpr (W > 1) {
     if (lane == 0) sums[wave] = s;
@@ -400,7 +464,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(Logprobs
     if (wave != 0) return;
     s = lane < W ? sums[lane < W ? lane : 0] : Sums{0.0, 0.0f, 0.0f};
     s = lanes_joined(s);
-    if constexpr (TOP) top = select_keys(&keys[0][0], W * a.top_k, BNN_MAX_ALTERNATIVES, a.top_k);
+    if constexpr (TOP) top = select_keys(&keys[0][0], W * a.top_k, BNN_MAX_ALTERNATIVES, a.top_k, slots[0]);
   }
   const uint64_t key = static_cast<uint64_t>(top.hi) << 32 | top.lo;
   if (splits == 1) {
@@ -426,10 +490,11 @@ __global__ __launch_bounds__(64) void join_kernel(LogprobsArgs a, int splits) {
     more = lanes_joined(more);
     s = p0 == 0 ? more : joined(s, more);
   }
-  Top top = {0, 0, 0, 0};
+  __shared__ uint64_t slots[64];
+  Top top = {0, 0, 0, 0, slots};
   if (a.top_k > 0)
     top = select_keys(reinterpret_cast<const uint64_t*>(at + sizeof(Part)), splits * a.top_k, bytes / 8,
-                      a.top_k);
+                      a.top_k, slots);
   write_row<T>(a, t, s, static_cast<uint64_t>(top.hi) << 32 | top.lo, factor_of(a.scale));
 }
 
