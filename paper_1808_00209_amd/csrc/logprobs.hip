@@ -140,20 +140,43 @@ struct Top {
   }
 };
 
-// Raises top.floor to an order that the values of at least top_k lanes reach
-// (mine: a lane's largest, 0 for none): ten bits of it below those that all
-// lanes' have in common, a lower bound of the top_k-th being all that is asked.
-__device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) {
+// An order that the values of at least `count` lanes reach (mine: a lane's
+// largest, 0 for none), or 0: ten bits of it below those that all lanes' have in
+// common, a lower bound of the count-th being all that is asked.
+__device__ __forceinline__ uint32_t reached_by(uint32_t mine, int count) {
   const uint32_t most = wave_max(mine), least = wave_min(mine ? mine : ~0u);
   const int own = most == least ? 0 : 32 - __builtin_clz(most ^ least);  // bits
   uint32_t at = own < 32 ? most >> own << own : 0;
-  if (__popcll(__ballot(mine >= at && mine != 0)) < top_k) return;
+  if (__popcll(__ballot(mine >= at && mine != 0)) < count) return 0;
   for (int b = own - 1; b >= 0 && b >= own - 10; --b) {
     const uint32_t next = at | 1u << b;
-    if (__popcll(__ballot(mine >= next)) >= top_k) at = next;
+    if (__popcll(__ballot(mine >= next)) >= count) at = next;
   }
+  return at;
+}
+__device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) {
+  const uint32_t at = reached_by(mine, top_k);
   if (at > top.floor) top.floor = at;
 }
+
+// W waves that share a row: each says what order its `each`-th largest value has
+// reached, and all of them have top_k values from the least of these on.  Read
+// without a wait for the others: what they said before is lower.
+template <int W>
+struct Shared {
+  uint32_t* said;  // [W], in LDS
+  int each;        // ceil(top_k / W)
+
+  __device__ __forceinline__ uint32_t floor() const {
+    if constexpr (W == 1) return 0;
+    const int lane = threadIdx.x & 63;
+    const uint32_t v = lane < W ? __atomic_load_n(&said[lane < W ? lane : 0], __ATOMIC_RELAXED) : ~0u;
+    return wave_min(v);
+  }
+  __device__ __forceinline__ void say(int wave, uint32_t order) const {
+    if (W > 1 && (threadIdx.x & 63) == 0) __atomic_store_n(&said[wave], order, __ATOMIC_RELAXED);
+  }
+};
 
 // SAFE: the reference is the largest value itself and differences are taken
 // before the factor, for rows whose c v leave fp32's range, rows without a value
@@ -218,10 +241,11 @@ __device__ __forceinline__ Sums joined(const Sums& a, const Sums& b) {
           fa * __builtin_fmaf(ma, a.s1, a.s2) + fb * __builtin_fmaf(mb, b.s1, b.s2)};
 }
 
-// Values [begin, end) of a row, by wave `wave` of `waves`.
-template <class T, bool SAFE, bool TOP>
-__device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave, int waves,
-                                     float c, int top_k, Top& top) {
+// Values [begin, end) of a row, by wave `wave` of W.
+template <class T, bool SAFE, bool TOP, int W>
+__device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave, float c, int top_k,
+                                     Top& top, const Shared<W>& shared) {
+  constexpr int waves = W;
   using R = typename RawOf<T>::type;
   constexpr bool kInts = std::is_same<R, int32_t>::value;
   constexpr int kGroups = kEach / 8;
@@ -251,7 +275,14 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
     sc.template add<kInts && !kPart>(f, some ? static_cast<float>(m) : -__builtin_inff());
     if constexpr (TOP) {
       const uint32_t mo = some ? order_of(m) : 0u;
-      const uint64_t reach = __ballot(some && mo >= top.floor);
+      uint64_t reach = __ballot(some && mo >= top.floor);
+      if (W > 1 && reach) {
+        const uint32_t floor = shared.floor();
+        if (floor > top.floor) {
+          top.floor = floor;
+          reach = __ballot(some && mo >= floor);
+        }
+      }
       if (reach) {
         if (__popcll(reach) > 12) raise_floor(top, mo, top_k);
         R floor;
@@ -269,6 +300,7 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
           }
           if (empty && count <= 64) {
             top.fill(count, top_k);
+            shared.say(wave, __builtin_amdgcn_readlane(top.hi, shared.each - 1));
             return;
           }
         }
@@ -287,6 +319,7 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
             }
           }
         }
+        shared.say(wave, __builtin_amdgcn_readlane(top.hi, shared.each - 1));
       }
     }
   };
@@ -330,13 +363,38 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
 }
 
 // A wave's sums: in fp32's range by the quick form, or else by the safe one.
-template <class T, bool TOP>
-__device__ __forceinline__ Sums wave_part(const T* row, int begin, int end, int wave, int waves,
-                                          float c, int top_k, Top& top) {
-  Sums s = scan<T, false, TOP>(row, begin, end, wave, waves, c, top_k, top);
+template <class T, bool TOP, int W>
+__device__ __forceinline__ Sums wave_part(const T* row, int begin, int end, int wave, float c, int top_k,
+                                          Top& top, const Shared<W>& shared) {
+  Sums s = scan<T, false, TOP>(row, begin, end, wave, c, top_k, top, shared);
   if (!(s.s1 > 0.0f && s.s1 < __builtin_inff()))
-    s = scan<T, true, false>(row, begin, end, wave, waves, c, top_k, top);
+    s = scan<T, true, false>(row, begin, end, wave, c, top_k, top, shared);
   return s;
+}
+
+// What the wave's first values let it say, before any is looked at closely.
+template <class T, int W>
+__device__ __forceinline__ void say_first(const T* row, int begin, int end, int wave,
+                                          const Shared<W>& shared) {
+  using R = typename RawOf<T>::type;
+  const int lane = threadIdx.x & 63, at = begin + wave * kStep;
+  uint32_t order = 0;
+  if (at + kStep <= end) {
+    R most = 0;
+#pragma unroll
+    for (int g = 0; g < kEach / 8; ++g) {
+      const Eight<T> e = load8(row + at + 512 * g + 8 * lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const R v = static_cast<R>(e.v[i]);
+        if (g + i == 0) most = v;
+        else if constexpr (std::is_same<R, float>::value) most = __builtin_fmaxf(most, v);
+        else most = most > v ? most : v;
+      }
+    }
+    order = reached_by(order_of(most), shared.each);
+  }
+  shared.say(wave, order);
 }
 
 // The top_k largest of `count` keys in lists of top_k, `stride` apart (0: none),
@@ -456,7 +514,15 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(Logprobs
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
   const float c = factor_of(a.scale);
   Top top = {0, 0, kFloor<R>, 0, slots[id]};
-  Sums s = wave_part<T, TOP>(row, begin, end, wave, W, c, a.top_k, top);
+  __shared__ uint32_t said[W];
+  const Shared<W> shared = {said, (a.top_k + W - 1) / W};
+  if constexpr (W > 1 && TOP) {
+    say_first(row, begin, end, wave, shared);
+    __syncthreads();
+    const uint32_t floor = shared.floor();
+    if (floor > top.floor) top.floor = floor;
+  }
+  Sums s = wave_part<T, TOP>(row, begin, end, wave, c, a.top_k, top, shared);
   if constexpr (W > 1) {
     if (lane == 0) sums[wave] = s;
     if (TOP && lane < a.top_k) keys[wave][lane] = static_cast<uint64_t>(top.hi) << 32 | top.lo;
@@ -501,7 +567,7 @@ __global__ __launch_bounds__(64) void join_kernel(LogprobsArgs a, int splits) {
 // Rows that fill the card with a workgroup each; fewer are split.
 constexpr int kFull = 256;
 constexpr int kParts = 1024;       // parts that fill it
-constexpr int kLength = 4 * kStep; // a part's values, at least
+constexpr int kLength = 16 * kStep; // a part's values, at least
 
 int64_t most_splits(int32_t V) { return (V + kLength - 1) / kLength; }
 int64_t splits_of(int64_t T, int32_t V) {
@@ -534,7 +600,7 @@ hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t s) {
     };
     auto waves = [&](auto tc) {
       if (a.V <= 4096) with(std::integral_constant<int, 1>{}, tc);
-      else if (splits == 1 && a.T < 2 * kParts && a.V >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
+      else if (a.T < 2 * kParts && length >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
       else with(std::integral_constant<int, 4>{}, tc);
     };
     if (a.top_k > 0) waves(std::true_type{});
