@@ -34,12 +34,9 @@ struct Sums {
   float s1, s2;
 };
 
-struct alignas(16) Part {  // followed by top_k keys
-  Sums sums;
-};
-__host__ __device__ inline size_t part_bytes(int top_k) {
-  return (sizeof(Part) + size_t{8} * top_k + 15) / 16 * 16;
-}
+// The workspace: a part's sums each, then top_k keys each.
+static_assert(sizeof(Sums) == 16, "as the workspace's size counts them");
+size_t part_bytes(int top_k) { return sizeof(Sums) + size_t{8} * top_k; }
 
 template <class T> struct RawOf { using type = float; };
 template <> struct RawOf<int32_t> { using type = int32_t; };
@@ -140,43 +137,20 @@ struct Top {
   }
 };
 
-// An order that the values of at least `count` lanes reach (mine: a lane's
-// largest, 0 for none), or 0: ten bits of it below those that all lanes' have in
-// common, a lower bound of the count-th being all that is asked.
-__device__ __forceinline__ uint32_t reached_by(uint32_t mine, int count) {
+// Raises top.floor to an order that the values of at least top_k lanes reach
+// (mine: a lane's largest, 0 for none): ten bits of it below those that all
+// lanes' have in common, a lower bound of the top_k-th being all that is asked.
+__device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) {
   const uint32_t most = wave_max(mine), least = wave_min(mine ? mine : ~0u);
   const int own = most == least ? 0 : 32 - __builtin_clz(most ^ least);  // bits
   uint32_t at = own < 32 ? most >> own << own : 0;
-  if (__popcll(__ballot(mine >= at && mine != 0)) < count) return 0;
+  if (__popcll(__ballot(mine >= at && mine != 0)) < top_k) return;
   for (int b = own - 1; b >= 0 && b >= own - 10; --b) {
     const uint32_t next = at | 1u << b;
-    if (__popcll(__ballot(mine >= next)) >= count) at = next;
+    if (__popcll(__ballot(mine >= next)) >= top_k) at = next;
   }
-  return at;
-}
-__device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) {
-  const uint32_t at = reached_by(mine, top_k);
   if (at > top.floor) top.floor = at;
 }
-
-// W waves that share a row: each says what order its `each`-th largest value has
-// reached, and all of them have top_k values from the least of these on.  Read
-// without a wait for the others: what they said before is lower.
-template <int W>
-struct Shared {
-  uint32_t* said;  // [W], in LDS
-  int each;        // ceil(top_k / W)
-
-  __device__ __forceinline__ uint32_t floor() const {
-    if constexpr (W == 1) return 0;
-    const int lane = threadIdx.x & 63;
-    const uint32_t v = lane < W ? __atomic_load_n(&said[lane < W ? lane : 0], __ATOMIC_RELAXED) : ~0u;
-    return wave_min(v);
-  }
-  __device__ __forceinline__ void say(int wave, uint32_t order) const {
-    if (W > 1 && (threadIdx.x & 63) == 0) __atomic_store_n(&said[wave], order, __ATOMIC_RELAXED);
-  }
-};
 
 // SAFE: the reference is the largest value itself and differences are taken
 // before the factor, for rows whose c v leave fp32's range, rows without a value
@@ -244,8 +218,7 @@ __device__ __forceinline__ Sums joined(const Sums& a, const Sums& b) {
 // Values [begin, end) of a row, by wave `wave` of W.
 template <class T, bool SAFE, bool TOP, int W>
 __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave, float c, int top_k,
-                                     Top& top, const Shared<W>& shared) {
-  constexpr int waves = W;
+                                     Top& top) {
   using R = typename RawOf<T>::type;
   constexpr bool kInts = std::is_same<R, int32_t>::value;
   constexpr int kGroups = kEach / 8;
@@ -275,14 +248,7 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
     sc.template add<kInts && !kPart>(f, some ? static_cast<float>(m) : -__builtin_inff());
     if constexpr (TOP) {
       const uint32_t mo = some ? order_of(m) : 0u;
-      uint64_t reach = __ballot(some && mo >= top.floor);
-      if (W > 1 && reach) {
-        const uint32_t floor = shared.floor();
-        if (floor > top.floor) {
-          top.floor = floor;
-          reach = __ballot(some && mo >= floor);
-        }
-      }
+      const uint64_t reach = __ballot(some && mo >= top.floor);
       if (reach) {
         if (__popcll(reach) > 12) raise_floor(top, mo, top_k);
         R floor;
@@ -300,7 +266,6 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
           }
           if (empty && count <= 64) {
             top.fill(count, top_k);
-            shared.say(wave, __builtin_amdgcn_readlane(top.hi, shared.each - 1));
             return;
           }
         }
@@ -319,7 +284,6 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
             }
           }
         }
-        shared.say(wave, __builtin_amdgcn_readlane(top.hi, shared.each - 1));
       }
     }
   };
@@ -333,7 +297,7 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
     for (int i = 0; i < kEach; ++i) v[i] = static_cast<R>(e[i / 8].v[i % 8]);
   };
   int at = begin + wave * kStep;
-  for (; at + kStep <= end; at += waves * kStep) {
+  for (; at + kStep <= end; at += W * kStep) {
     Eight<T> e[kGroups];
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) e[g] = load8(row + at + 512 * g + 8 * lane);
@@ -365,65 +329,45 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
 // A wave's sums: in fp32's range by the quick form, or else by the safe one.
 template <class T, bool TOP, int W>
 __device__ __forceinline__ Sums wave_part(const T* row, int begin, int end, int wave, float c, int top_k,
-                                          Top& top, const Shared<W>& shared) {
-  Sums s = scan<T, false, TOP>(row, begin, end, wave, c, top_k, top, shared);
+                                          Top& top) {
+  Sums s = scan<T, false, TOP, W>(row, begin, end, wave, c, top_k, top);
   if (!(s.s1 > 0.0f && s.s1 < __builtin_inff()))
-    s = scan<T, true, false>(row, begin, end, wave, c, top_k, top, shared);
+    s = scan<T, true, false, W>(row, begin, end, wave, c, top_k, top);
   return s;
 }
 
-// What the wave's first values let it say, before any is looked at closely.
-template <class T, int W>
-__device__ __forceinline__ void say_first(const T* row, int begin, int end, int wave,
-                                          const Shared<W>& shared) {
-  using R = typename RawOf<T>::type;
-  const int lane = threadIdx.x & 63, at = begin + wave * kStep;
-  uint32_t order = 0;
-  if (at + kStep <= end) {
-    R most = 0;
-#pragma unroll
-    for (int g = 0; g < kEach / 8; ++g) {
-      const Eight<T> e = load8(row + at + 512 * g + 8 * lane);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const R v = static_cast<R>(e.v[i]);
-        if (g + i == 0) most = v;
-        else if constexpr (std::is_same<R, float>::value) most = __builtin_fmaxf(most, v);
-        else most = most > v ? most : v;
-      }
-    }
-    order = reached_by(order_of(most), shared.each);
-  }
-  shared.say(wave, order);
-}
-
-// The top_k largest of `count` keys in lists of top_k, `stride` apart (0: none),
-// by one wave.
-__device__ __forceinline__ Top select_keys(const uint64_t* keys, int count, int stride, int top_k,
-                                           uint64_t* slots) {
+// The top_k largest of `count` keys (0: none), by one wave.
+__device__ __forceinline__ Top select_keys(const uint64_t* keys, int count, int top_k, uint64_t* slots) {
   const int lane = threadIdx.x & 63;
-  auto at = [&](int i) {
-    const int list = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(top_k));
-    return i < count ? keys[list * stride + i - list * top_k] : uint64_t{0};
-  };
-  Top top = {0, 0, 0, 0, slots};
+  constexpr int kHeld = 4;  // a lane's keys in registers, others are read again
+  uint64_t held[kHeld];
   uint32_t most = 0;
-  for (int i = lane; i < count; i += 64) {
-    const uint32_t o = static_cast<uint32_t>(at(i) >> 32);
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    held[j] = 64 * j + lane < count ? keys[64 * j + lane] : 0;
+    const uint32_t o = static_cast<uint32_t>(held[j] >> 32);
     most = most > o ? most : o;
   }
+  for (int i = 64 * kHeld + lane; i < count; i += 64) {
+    const uint32_t o = static_cast<uint32_t>(keys[i] >> 32);
+    most = most > o ? most : o;
+  }
+  Top top = {0, 0, 0, 0, slots};
   raise_floor(top, most, top_k);
   int collected = 0;
-  for (int i0 = 0; i0 < count; i0 += 64) {
-    const uint64_t key = at(i0 + lane);
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    top.collect(held[j], held[j] != 0 && static_cast<uint32_t>(held[j] >> 32) >= top.floor, collected);
+  for (int i0 = 64 * kHeld; i0 < count; i0 += 64) {
+    const uint64_t key = i0 + lane < count ? keys[i0 + lane] : 0;
     top.collect(key, key != 0 && static_cast<uint32_t>(key >> 32) >= top.floor, collected);
   }
   if (collected <= 64) {
     top.fill(collected, top_k);
     return top;
   }
-  for (int i0 = 0; i0 < count; i0 += 64) {
-    const uint64_t key = at(i0 + lane);
+  for (int i0 = 0; i0 < count; i0 += 64) {  // (many equal ones)
+    const uint64_t key = i0 + lane < count ? keys[i0 + lane] : 0;
     const uint32_t hi = static_cast<uint32_t>(key >> 32), lo = static_cast<uint32_t>(key);
     uint64_t mask = __ballot(hi >= top.floor && key > top.bound);
     while (mask) {
@@ -500,7 +444,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(Logprobs
                                                                         int length) {
   using R = typename RawOf<T>::type;
   __shared__ Sums sums[W];
-  __shared__ uint64_t keys[W][BNN_MAX_ALTERNATIVES];
+  __shared__ uint64_t keys[W * BNN_MAX_ALTERNATIVES];
   __shared__ uint64_t slots[W > 4 ? W : 4][64];
   constexpr int kParts = W > 4 ? 1 : 4 / W;  // of a workgroup
   const int lane = threadIdx.x & 63;
@@ -514,60 +458,51 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(Logprobs
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
   const float c = factor_of(a.scale);
   Top top = {0, 0, kFloor<R>, 0, slots[id]};
-  __shared__ uint32_t said[W];
-  const Shared<W> shared = {said, (a.top_k + W - 1) / W};
-  if constexpr (W > 1 && TOP) {
-    say_first(row, begin, end, wave, shared);
-    __syncthreads();
-    const uint32_t floor = shared.floor();
-    if (floor > top.floor) top.floor = floor;
-  }
-  Sums s = wave_part<T, TOP>(row, begin, end, wave, c, a.top_k, top, shared);
+  Sums s = wave_part<T, TOP, W>(row, begin, end, wave, c, a.top_k, top);
   if constexpr (W > 1) {
     if (lane == 0) sums[wave] = s;
-    if (TOP && lane < a.top_k) keys[wave][lane] = static_cast<uint64_t>(top.hi) << 32 | top.lo;
+    if (TOP && lane < a.top_k) keys[wave * a.top_k + lane] = static_cast<uint64_t>(top.hi) << 32 | top.lo;
     __syncthreads();
     if (wave != 0) return;
     s = lane < W ? sums[lane < W ? lane : 0] : Sums{0.0, 0.0f, 0.0f};
     s = lanes_joined(s);
-    if constexpr (TOP) top = select_keys(&keys[0][0], W * a.top_k, BNN_MAX_ALTERNATIVES, a.top_k, slots[0]);
+    if constexpr (TOP) top = select_keys(keys, W * a.top_k, a.top_k, slots[0]);
   }
   const uint64_t key = static_cast<uint64_t>(top.hi) << 32 | top.lo;
   if (splits == 1) {
     write_row<T>(a, t, s, key, c);
   } else {
-    char* out = static_cast<char*>(a.workspace) + part * part_bytes(a.top_k);
-    if (lane == 0) reinterpret_cast<Part*>(out)->sums = s;
-    if (TOP && lane < a.top_k) reinterpret_cast<uint64_t*>(out + sizeof(Part))[lane] = key;
+    Sums* all = static_cast<Sums*>(a.workspace);
+    if (lane == 0) all[part] = s;
+    if (TOP && lane < a.top_k)
+      reinterpret_cast<uint64_t*>(all + a.T * splits)[part * a.top_k + lane] = key;
   }
 }
 
 // A row's parts put together, by one wave.
 template <class T>
 __global__ __launch_bounds__(64) void join_kernel(LogprobsArgs a, int splits) {
+  __shared__ uint64_t slots[64];
   const int64_t t = blockIdx.x;
-  const int bytes = static_cast<int>(part_bytes(a.top_k));
-  const char* at = static_cast<const char*>(a.workspace) + t * splits * bytes;
+  const Sums* all = static_cast<const Sums*>(a.workspace);
+  const uint64_t* keys = reinterpret_cast<const uint64_t*>(all + a.T * splits) + t * splits * a.top_k;
   Sums s = {0.0, 0.0f, 0.0f};
   for (int p0 = 0; p0 < splits; p0 += 64) {
     const int p = p0 + static_cast<int>(threadIdx.x);
     Sums more = {0.0, 0.0f, 0.0f};
-    if (p < splits) more = reinterpret_cast<const Part*>(at + p * bytes)->sums;
+    if (p < splits) more = all[t * splits + p];
     more = lanes_joined(more);
     s = p0 == 0 ? more : joined(s, more);
   }
-  __shared__ uint64_t slots[64];
-  Top top = {0, 0, 0, 0, slots};
-  if (a.top_k > 0)
-    top = select_keys(reinterpret_cast<const uint64_t*>(at + sizeof(Part)), splits * a.top_k, bytes / 8,
-                      a.top_k, slots);
+  Top top = {};
+  if (a.top_k > 0) top = select_keys(keys, splits * a.top_k, a.top_k, slots);
   write_row<T>(a, t, s, static_cast<uint64_t>(top.hi) << 32 | top.lo, factor_of(a.scale));
 }
 
 // Rows that fill the card with a workgroup each; fewer are split.
 constexpr int kFull = 256;
 constexpr int kParts = 1024;       // parts that fill it
-constexpr int kLength = 16 * kStep; // a part's values, at least
+constexpr int kLength = 4 * kStep;  // a part's values, at least
 
 int64_t most_splits(int32_t V) { return (V + kLength - 1) / kLength; }
 int64_t splits_of(int64_t T, int32_t V) {
@@ -600,7 +535,7 @@ hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t s) {
     };
     auto waves = [&](auto tc) {
       if (a.V <= 4096) with(std::integral_constant<int, 1>{}, tc);
-      else if (a.T < 2 * kParts && length >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
+      else if (splits == 1 && a.T < 2 * kFull && a.V >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
       else with(std::integral_constant<int, 4>{}, tc);
     };
     if (a.top_k > 0) waves(std::true_type{});

@@ -11,6 +11,7 @@
 // is rounded as it is.
 #include "dtypes.hpp"
 #include "quant.hpp"
+#include "wave_ops.hpp"
 
 namespace bnn {
 namespace {
@@ -61,17 +62,6 @@ __device__ __forceinline__ void store8(T* p, const Eight<T>& e, int n) {
     for (int i = 0; i < 8; ++i)
       if (i < n) p[i] = e.v[i];
   }
-}
-
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
-  return v;
-}
-__device__ __forceinline__ double wave_max(double v) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) v = fmax(v, __shfl_xor(v, o));
-  return v;
 }
 
 // The row's totals over its W waves (in a workgroup of 4 / W rows, or of W waves).
@@ -220,6 +210,9 @@ void launch_types(const NormArgs& a, hipStream_t s) {
     rmsnorm_kernel<T, TW, W, G><<<grid, W > 4 ? W * 64 : kNT, 0, s>>>(a);
   };
   const int groups = (a.D + 7) / 8;
+#ifdef NORM_FORCE
+  return go(std::integral_constant<int, NORM_W>{}, std::integral_constant<int, NORM_G>{});
+#endif
   using std::integral_constant;
   if (groups <= 64) return go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
   if (groups <= 256) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
