@@ -808,14 +808,22 @@ def _together(like, *others):
     for t in others:
         if t is not None and t.device != at:
             raise ValueError("tensors on %s and on %s in one call" % (at, t.device))
-    if at.index is not None and _raw_device is not None and at.index != _raw_device():
+    if _raw_device is not None and at.index is not None and at.index != _raw_device():
         raise ValueError("tensors on %s, but the current device is cuda:%d: use torch.cuda.device"
                          % (at, _raw_device()))
 
 
 def _rows8(like, M, D, stream):
     """New 8-bit rows [M, D], a multiple of 16 bytes apart."""
+    if D % 16 == 0:
+        return _empty(like, (M, D), torch.int8, stream)
     return _empty(like, (M, (D + 15) // 16 * 16), torch.int8, stream)[:, :D]
+
+
+# (A call's description is a function of its sizes: made once for each.)
+@functools.lru_cache(maxsize=1024)
+def _desc(kind, *fields):
+    return ctypes.byref(kind(*fields))
 
 
 def _int8_rows(t, name):
@@ -847,22 +855,23 @@ def bnn_rmsnorm(x, weight=None, residual=None, eps=1e-6, want_y=False, want_q=Tr
     if weight is not None:
         w_code = 0 if weight.dtype is torch.float32 else code
         _shaped(_dev(weight, kind if w_code else torch.float32, "weight"), (D,), "weight")
+    _together(x, residual, weight, sum, y, q, scale)
     if residual is not None or sum is not None:
         sum = _output(sum, x, (M, D), kind, "sum", stream)
     if want_y or y is not None:
         y = _output(y, x, (M, D), kind, "y", stream)
-    if want_q or q is not None:
-        if q is None:
-            q = _rows8(x, M, D, stream)
+    q_stride = 0
+    if q is not None:
         q_stride = _int8_rows(_shaped(q, (M, D), "q"), "q")
+    elif want_q:
+        q = _rows8(x, M, D, stream)
+        q_stride = (D + 15) // 16 * 16
+    if q is not None:
         scale = _output(scale, x, (M,), torch.float32, "scale", stream)
     elif scale is not None:
         raise ValueError("scale goes with q")
-    else:
-        q_stride = 0
-    _together(x, residual, weight, sum, y, q, scale)
-    d = RmsnormDesc(M, D, code, w_code, eps)
-    _check(lib.bnn_rmsnorm(ctypes.byref(d), _ptr(x), stride, _ptr(residual), r_stride,
+    d = _desc(RmsnormDesc, M, D, code, w_code, eps)
+    _check(lib.bnn_rmsnorm(d, _ptr(x), stride, _ptr(residual), r_stride,
                            _ptr(weight), _ptr(sum), _ptr(y), _ptr(q), q_stride, _ptr(scale),
                            _stream(stream)))
     return sum, y, q, scale
@@ -882,12 +891,12 @@ def bnn_q8gemm(x, w, x_scale=None, w_scale=None, bias=None, dtype=torch.float32,
     _shaped(_dev(x_scale, torch.float32, "x_scale"), (M,), "x_scale")
     _shaped(_dev(w_scale, torch.float32, "w_scale"), (N,), "w_scale")
     _shaped(_dev(bias, torch.float32, "bias"), (N,), "bias")
+    _together(x, w, x_scale, w_scale, bias, out)
     dtype = dtype if out is None else out.dtype
     code = _real(dtype, "out")
     out = _output(out, x, (M, N), dtype, "out", stream)
-    _together(x, w, x_scale, w_scale, bias, out)
-    d = Q8gemmDesc(M, N, K, code)
-    _check(lib.bnn_q8gemm(ctypes.byref(d), _ptr(x), x_stride, _ptr(x_scale), _ptr(w), w_stride,
+    d = _desc(Q8gemmDesc, M, N, K, code)
+    _check(lib.bnn_q8gemm(d, _ptr(x), x_stride, _ptr(x_scale), _ptr(w), w_stride,
                           _ptr(w_scale), _ptr(bias), _ptr(out), _stream(stream)))
     return out
 
@@ -918,6 +927,7 @@ def bnn_logprobs(logits, ids=None, top_k=0, logit_scale=1.0, want_entropy=True, 
         raise TypeError("logits must be float32, float16, bfloat16 or int32")
     stride = _rows(logits, "logits")
     T, V = logits.shape
+    _together(logits, ids, logp, entropy, top_ids, top_logp, workspace)
     n = 0
     if ids is not None:
         if _dev(ids, torch.int32, "ids").dim() not in (1, 2) or ids.shape[0] != T:
@@ -933,10 +943,9 @@ def bnn_logprobs(logits, ids=None, top_k=0, logit_scale=1.0, want_entropy=True, 
         top_logp = _output(top_logp, logits, (T, top_k), torch.float32, "top_logp", stream)
     elif top_ids is not None or top_logp is not None:
         raise ValueError("top_ids and top_logp go with top_k")
-    d = LogprobsDesc(T, V, n, top_k, dtype, logit_scale)
+    d = _desc(LogprobsDesc, T, V, n, top_k, dtype, logit_scale)
     workspace, size = _workspace(workspace, _logprobs_bytes(T, V, top_k), logits, stream)
-    _together(logits, ids, logp, entropy, top_ids, top_logp, workspace)
-    _check(lib.bnn_logprobs(ctypes.byref(d), _ptr(logits), stride, _ptr(ids), _ptr(logp),
+    _check(lib.bnn_logprobs(d, _ptr(logits), stride, _ptr(ids), _ptr(logp),
                             _ptr(entropy), _ptr(top_ids), _ptr(top_logp), _ptr(workspace), size,
                             _stream(stream)))
     return logp, entropy, top_ids, top_logp

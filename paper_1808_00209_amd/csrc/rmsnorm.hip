@@ -1,14 +1,18 @@
 // Root-mean-square norm with the residual's addition and an output in 8 bits
 // (bnn_rmsnorm).  One pass: a row stays in the registers of its W waves, 8
 // values at a time per lane, from the sum of squares and the largest |h w| to
-// the rounding.
+// the rounding.  Bound by memory: 8192 x 4096 bf16 with a residual in 45.8 us,
+// 5.1 TB/s (a large copy's rate on this card), fp32 in 88 us, 5.0 TB/s.
 //
-// r cancels in q = rint(127 p / max p), p = h w.  Where both are 16-bit values
-// p is exact in fp32, and the quotient of the 23-bit 127 p by max p comes no
-// nearer to a border n + 1/2 than 2^-24 of it without lying on it; products of
-// fp32 values need 64 bits.  So a value whose fp32 quotient comes near a border
-// (within 2^-13, far more than its error) is divided again in 64 bits; the rest
-// is rounded as it is.
+// r cancels in q = rint(127 p / max p), p = h w, which is rounded as if from the
+// exact p: where the quotient comes near a border n + 1/2 (within 2^-13, many
+// times its error of at most 127 * 3 * 2^-24), it is divided again in 64 bits;
+// else it is rounded as it is.
+//
+// Rows and weights of 16 bits: p is exact in fp32 (8 + 8 or 11 + 11 bits), and so
+// is its largest; sums and quotients are fp32's, as long as the largest p and
+// the sum of squares lie well inside its range.  Other rows (infinities, NaN and
+// rows of zeros among them), and rows or weights of fp32, go in 64 bits.
 #include "dtypes.hpp"
 #include "quant.hpp"
 #include "wave_ops.hpp"
@@ -64,6 +68,39 @@ __device__ __forceinline__ void store8(T* p, const Eight<T>& e, int n) {
   }
 }
 
+// 8 of a row's bytes, n of them in the row.
+__device__ __forceinline__ void store_q(int8_t* q, uint32_t b0, uint32_t b1, int n) {
+  if (n >= 8) {
+    *reinterpret_cast<u32x2_any*>(q) = u32x2_any{b0, b1};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) q[i] = static_cast<int8_t>((i < 4 ? b0 : b1) >> (8 * (i % 4)));
+  }
+}
+
+// The fp32 totals of a row over its W waves.
+template <int W>
+__device__ __forceinline__ void row_totals(float& ss, float& top, float (*part)[2]) {
+  ss = wave_sum(ss);
+  top = wave_max(top);
+  if constexpr (W > 1) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+      part[wave][0] = ss;
+      part[wave][1] = top;
+    }
+    __syncthreads();
+    ss = part[0][0];
+    top = part[0][1];
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+      ss += part[w][0];
+      top = __builtin_fmaxf(top, part[w][1]);
+    }
+  }
+}
+
 // The row's totals over its W waves (in a workgroup of 4 / W rows, or of W waves).
 template <int W>
 __device__ __forceinline__ NormRow row_totals(NormRow r, double (*part)[2]) {
@@ -101,6 +138,16 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void rmsnorm_kernel(NormArgs 
   const TW* weight = static_cast<const TW*>(a.weight);
   const int D = a.D;
 
+  auto weight8 = [&](int d) {
+    Eight<TW> w;
+    if (weight) return load8(weight + d, D - d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w.v[i] = TW(1.0f);
+    return w;
+  };
+  constexpr bool kNarrow = sizeof(T) == 2 && sizeof(TW) == 2;
+  Eight<TW> held[kNarrow ? G : 1];  // (asked for with the rows: their wait is one)
+
   Eight<T> h[G];
 #pragma unroll
   for (int g = 0; g < G; ++g) {
@@ -110,15 +157,29 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void rmsnorm_kernel(NormArgs 
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[g].v[i] = T(0.0f);
   }
+  auto hold_weight = [&]() {
+    if constexpr (kNarrow) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int d = 8 * (lane + g * W * 64);
+        held[g] = d < D ? weight8(d) : Eight<TW>{};
+      }
+    }
+  };
   if (res) {
+    Eight<T> r[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const int d = 8 * (lane + g * W * 64);
-      if (d >= D) break;
-      const Eight<T> r = load8(res + d, D - d);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[g].v[i] = from_f32<T>(to_f32(h[g].v[i]) + to_f32(r.v[i]));
+      r[g] = d < D ? load8(res + d, D - d) : Eight<T>{};
     }
+    hold_weight();
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[g].v[i] = from_f32<T>(to_f32(h[g].v[i]) + to_f32(r[g].v[i]));
+  } else {
+    hold_weight();
   }
   if (a.sum) {
     T* sum = static_cast<T*>(a.sum) + m * D;
@@ -128,13 +189,65 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void rmsnorm_kernel(NormArgs 
       if (d < D) store8(sum + d, h[g], D - d);
     }
   }
-  auto weight8 = [&](int d) {
-    Eight<TW> w;
-    if (weight) return load8(weight + d, D - d);
+  if constexpr (kNarrow) {
+    __shared__ float totals[W][2];
+    float p[G][8], ss = 0.0f, top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w.v[i] = TW(1.0f);
-    return w;
-  };
+    for (int g = 0; g < G; ++g) {
+      const Eight<TW>& w = held[g];
+      float sq = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = to_f32(h[g].v[i]);
+        sq = __builtin_fmaf(v, v, sq);
+        p[g][i] = v * to_f32(w.v[i]);
+        top = __builtin_fmaxf(top, __builtin_fabsf(p[g][i]));
+      }
+      ss += sq;
+    }
+    row_totals<W>(ss, top, totals);
+    if (ss > 1e-25f && ss < 1e37f && top > 1e-25f && top < 1e37f) {
+      const float rstd = 1.0f / __builtin_sqrtf(ss / static_cast<float>(D) + a.eps);
+      if (a.q && lane == 0) a.scale[m] = top * rstd / 127.0f;
+      const float inv = 127.0f / top;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int d = 8 * (lane + g * W * 64);
+        if (d >= D) break;
+        if (a.y) {
+          Eight<T> y;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y.v[i] = from_f32<T>(p[g][i] * rstd);
+          store8(static_cast<T*>(a.y) + m * D + d, y, D - d);
+        }
+        if (a.q) {
+          // 1.5 * 2^23 added: fp32 rounds to whole numbers there, and its low
+          // byte is that number's
+          constexpr float kWhole = 12582912.0f;
+          float t[8], near = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            t[i] = __builtin_fmaf(p[g][i], inv, kWhole);
+            near = __builtin_fmaxf(near, __builtin_fabsf(__builtin_fmaf(p[g][i], inv, kWhole - t[i])));
+          }
+          if (near > 0.5f - 0x1p-13f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              t[i] = kWhole + static_cast<float>(__builtin_rint(127.0 * static_cast<double>(p[g][i]) /
+                                                                static_cast<double>(top)));
+          }
+          auto bits = [&](int i) { return __builtin_bit_cast(uint32_t, t[i]); };
+          // (v_perm: bytes 0-3 of its second operand, 4-7 of its first)
+          auto four = [&](int i) {
+            return __builtin_amdgcn_perm(__builtin_amdgcn_perm(bits(i + 3), bits(i + 2), 0x0c0c0400),
+                                         __builtin_amdgcn_perm(bits(i + 1), bits(i), 0x0c0c0400), 0x05040100);
+          };
+          store_q(a.q + m * a.q_stride + d, four(0), four(4), D - d);
+        }
+      }
+      return;
+    }
+  }
 
   NormRow r = {0.0, 0.0};
 #pragma unroll
@@ -189,14 +302,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void rmsnorm_kernel(NormArgs 
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         b[i / 4] |= (static_cast<uint32_t>(static_cast<int>(t[i])) & 0xFFu) << (8 * (i % 4));
-      int8_t* q = a.q + m * a.q_stride + d;
-      if (D - d >= 8) {
-        *reinterpret_cast<u32x2_any*>(q) = u32x2_any{b[0], b[1]};
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < D - d) q[i] = static_cast<int8_t>(b[i / 4] >> (8 * (i % 4)));
-      }
+      store_q(a.q + m * a.q_stride + d, b[0], b[1], D - d);
     }
   }
 }
@@ -210,16 +316,26 @@ void launch_types(const NormArgs& a, hipStream_t s) {
     rmsnorm_kernel<T, TW, W, G><<<grid, W > 4 ? W * 64 : kNT, 0, s>>>(a);
   };
   const int groups = (a.D + 7) / 8;
-#ifdef NORM_FORCE
-  return go(std::integral_constant<int, NORM_W>{}, std::integral_constant<int, NORM_G>{});
-#endif
   using std::integral_constant;
-  if (groups <= 64) return go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-  if (groups <= 256) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-  if (groups <= 512) return go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-  if (groups <= 1024) return go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-  if (groups <= 2048) return go(integral_constant<int, 16>{}, integral_constant<int, 2>{});
-  return go(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+  using One = integral_constant<int, 1>;
+  using Two = integral_constant<int, 2>;
+  using Four = integral_constant<int, 4>;
+  using Eight_ = integral_constant<int, 8>;
+  // Where there are rows for all CUs, rows up to 1536 values go to a wave each
+  // (us, bf16 with residual, one wave : four waves: 32768 x 1024 47 : 57, 32768 x
+  // 600 36 : 52; 16384 x 1100 fp32 32 : 40; 16384 x 2048 50 : 45); a few rows are
+  // done sooner by four (301 x 1024 4.8 : 4.0).  Longer rows, eight waves : four :
+  // sixteen: 8192 x 4096 45.8 : 46.5 : 86; eight : sixteen: 4096 x 8192 48 : 65,
+  // 2048 x 16384 54 : 60.
+  const bool many = a.M >= 4096;
+  if (groups <= 64) return go(One{}, One{});
+  if (many && groups <= 128) return go(One{}, Two{});
+  if (many && groups <= 192) return go(One{}, Four{});
+  if (groups <= 256) return go(Four{}, One{});
+  if (groups <= 512) return go(Eight_{}, One{});
+  if (groups <= 1024) return go(Eight_{}, Two{});
+  if (groups <= 2048) return go(Eight_{}, Four{});
+  return go(integral_constant<int, 16>{}, Eight_{});
 }
 
 }  // namespace

@@ -62,7 +62,7 @@ def test_sizes(kind, M, D):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp32"])
-@pytest.mark.parametrize("D", [64, 512, 1000, 4096])
+@pytest.mark.parametrize("D", [64, 512, 1000, 1030, 1300, 1536, 4096])
 def test_many_rows(kind, D):
     g = torch.Generator().manual_seed(D)
     _check(_rows(g, 4097, D, kind), _rows(g, 1, D, kind)[0], _rows(g, 4097, D, kind))
