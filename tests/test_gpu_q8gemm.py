@@ -54,7 +54,11 @@ SIZES = [(1, 1, 1), (1, 5, 3), (1, 16, 64), (1, 33, 100), (1, 4096, 4096), (1, 1
          # whole stages, and short last ones with whole chunks and without
          (1000, 4100, 100), (2000, 2000, 16), (1100, 3900, 1024), (1030, 3700, 1104), (2000, 4200, 31),
          (2000, 4100, 384), (2100, 4000, 400), (4100, 3900, 16), (3900, 4100, 256), (3850, 4000, 1029),
-         (4096, 4096, 640), (4000, 4001, 99)]
+         (4096, 4096, 640), (4000, 4001, 99), (300, 300, 400), (1050, 4000, 1029),
+         (1000, 4000, 100), (1000, 4000, 1024), (1000, 4001, 400), (990, 4000, 1029),
+         (2000, 4000, 31), (2000, 4001, 384), (2000, 4000, 400), (1950, 3999, 1029), (4000, 4001, 400),
+         # few rows of more than x's registers hold
+         (1, 70, 10000), (16, 100, 8208), (5, 64, 20011), (40, 70, 4112), (20, 4096, 4096)]
 
 
 @pytest.mark.parametrize("M, N, K", SIZES)
