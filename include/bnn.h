@@ -754,7 +754,7 @@ typedef struct bnn_logprobs_desc {
                      /* V)                                                   */
   int32_t dtype;     /* bnn_dtype of the logits                              */
   float logit_scale; /* factor on the logits (1 / temperature), positive and */
-                     /* finite                                               */
+                     /* at most 2^100                                        */
 } bnn_logprobs_desc;
 
 #define BNN_MAX_GIVEN 1024

@@ -27,7 +27,8 @@ constexpr int kNT = 256;  // unless a row has more waves
 constexpr int kEach = 16;           // values of a lane per step, in groups of 8
 constexpr int kStep = 64 * kEach;   // of a wave
 constexpr float kAway = 60.0f;
-constexpr float kFar = 3e38f;
+constexpr float kFar = 3e38f;    // the reference before there is one: minus this
+constexpr float kLarge = 0x1p20f; // the quick form's references, at most
 
 struct Sums {
   double ref;
@@ -153,8 +154,8 @@ __device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) 
 }
 
 // SAFE: the reference is the largest value itself and differences are taken
-// before the factor, for rows whose c v leave fp32's range, rows without a value
-// in reach and rows with NaN or infinity.
+// before the factor, for rows whose c v pass 2^20, rows without a value in reach
+// and rows with NaN or infinity (whose quick sums end as 0, NaN or infinity).
 template <bool SAFE>
 struct Scan {
   float c, ref, s1, s2;
@@ -173,9 +174,11 @@ struct Scan {
   __device__ __forceinline__ void add(const float (&v)[kEach], float fm) {
     if (__any(SAFE ? fm > ref : delta(fm) > kAway)) {
       const float top = wave_max(fm);
-      const float next = SAFE ? top : __builtin_fminf(__builtin_fmaxf(top * c, -kFar), kFar);
+      const float next = SAFE ? top : top * c;
+      // (a quick reference's own rounding must not count: 2^-5 at most)
+      if (!SAFE && !(__builtin_fabsf(next) <= kLarge)) s1 = __builtin_nanf("");
       float move = SAFE ? (ref - next) * c : ref - next;
-      move = s1 > 0.0f ? __builtin_fmaxf(move, -1e4f) : -1e4f;
+      move = s1 == 0.0f ? -1e4f : __builtin_fmaxf(move, -1e4f);
       const float f = exp2_of(move);
       s2 = f * __builtin_fmaf(move, s1, s2);
       s1 *= f;
@@ -336,16 +339,30 @@ __device__ __forceinline__ Sums wave_part(const T* row, int begin, int end, int 
   return s;
 }
 
-// The top_k largest of `count` keys (0: none), by one wave.
-__device__ __forceinline__ Top select_keys(const uint64_t* keys, int count, int top_k, uint64_t* slots) {
+// A lane's keys out of `count` (0: none): these in registers, others are read
+// again.
+constexpr int kHeld = 4;
+struct Held {
+  uint64_t key[kHeld];
+};
+__device__ __forceinline__ Held hold_keys(const uint64_t* keys, int count) {
+  Held h;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = 64 * j + static_cast<int>(threadIdx.x & 63);
+    h.key[j] = i < count ? keys[i] : 0;
+  }
+  return h;
+}
+
+// The top_k largest of `count` keys, by one wave.
+__device__ __forceinline__ Top select_keys(const Held& h, const uint64_t* keys, int count, int top_k,
+                                           uint64_t* slots) {
   const int lane = threadIdx.x & 63;
-  constexpr int kHeld = 4;  // a lane's keys in registers, others are read again
-  uint64_t held[kHeld];
   uint32_t most = 0;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
-    held[j] = 64 * j + lane < count ? keys[64 * j + lane] : 0;
-    const uint32_t o = static_cast<uint32_t>(held[j] >> 32);
+    const uint32_t o = static_cast<uint32_t>(h.key[j] >> 32);
     most = most > o ? most : o;
   }
   for (int i = 64 * kHeld + lane; i < count; i += 64) {
@@ -357,7 +374,7 @@ __device__ __forceinline__ Top select_keys(const uint64_t* keys, int count, int 
   int collected = 0;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
-    top.collect(held[j], held[j] != 0 && static_cast<uint32_t>(held[j] >> 32) >= top.floor, collected);
+    top.collect(h.key[j], h.key[j] != 0 && static_cast<uint32_t>(h.key[j] >> 32) >= top.floor, collected);
   for (int i0 = 64 * kHeld; i0 < count; i0 += 64) {
     const uint64_t key = i0 + lane < count ? keys[i0 + lane] : 0;
     top.collect(key, key != 0 && static_cast<uint32_t>(key >> 32) >= top.floor, collected);
@@ -392,38 +409,52 @@ __device__ __forceinline__ Sums lanes_joined(Sums s) {
           wave_sum(f * __builtin_fmaf(move, s.s1, s.s2))};
 }
 
+// The first 64 of a row's given answers, a lane's: asked for early, since the
+// logit waits for the id (ids first, then `gather`).
+template <class T>
+struct Given {
+  using R = typename RawOf<T>::type;
+  int id = -1;
+  R v = 0;
+  __device__ __forceinline__ void ask(const LogprobsArgs& a, int64_t t) {
+    const int lane = threadIdx.x & 63;
+    if (lane < a.n) id = a.ids[t * a.n + lane];
+  }
+  __device__ __forceinline__ void gather(const LogprobsArgs& a, int64_t t) {
+    if (id >= 0 && id < a.V) v = static_cast<R>(static_cast<const T*>(a.logits)[t * a.stride + id]);
+  }
+};
+
 // A row's outputs from its sums and (lane j: the j-th) keys, by one wave.
 template <class T>
 __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t t, const Sums& s,
-                                          uint64_t key, float c) {
+                                          uint64_t key, float c, Given<T> given) {
   using R = typename RawOf<T>::type;
   constexpr double kLn2 = 0.693147180559945309417;
   const int lane = threadIdx.x & 63;
   const bool none = s.s1 == 0.0f, bad = !(s.s1 < __builtin_inff());
   // (2^-60 <= s1 < 2^24 2^60, or 1 <= s1 <= 2^24 by the safe form)
   const float ls = __builtin_amdgcn_logf(s.s1);
-  const bool small = __builtin_fabs(s.ref) < 1e30;
   const float ref = static_cast<float>(s.ref);
+  const bool quick = static_cast<double>(ref) == s.ref && __builtin_fabsf(ref) <= kLarge;
   const float nan = __builtin_nanf("");
   auto ln_p = [&](R v) {
     if (std::is_same<R, float>::value && static_cast<float>(v) == -__builtin_inff())
       return -__builtin_inff();
     const float d = __builtin_fmaf(static_cast<float>(v), c, -ref);
-    if (small && __builtin_fabsf(d) < 1e30f) return (d - ls) * static_cast<float>(kLn2);
+    if (quick && __builtin_fabsf(d) < 1e30f) return (d - ls) * static_cast<float>(kLn2);
     return static_cast<float>((static_cast<double>(v) * c - s.ref - static_cast<double>(ls)) * kLn2);
   };
   if (a.entropy && lane == 0)
     a.entropy[t] = bad ? nan : none ? 0.0f
         : (ls - s.s2 / s.s1) * static_cast<float>(kLn2);
   for (int j = lane; j < a.n; j += 64) {
-    const int id = a.ids[t * a.n + j];
-    float lp = -__builtin_inff();
-    if (id >= 0 && id < a.V) {
-      const R v = static_cast<R>(static_cast<const T*>(a.logits)[t * a.stride + id]);
-      if (bad) lp = nan;
-      else if (!none) lp = ln_p(v);
+    if (j >= 64) {
+      given.id = a.ids[t * a.n + j];
+      given.gather(a, t);
     }
-    a.logp[t * a.n + j] = lp;
+    const bool there = given.id >= 0 && given.id < a.V;
+    a.logp[t * a.n + j] = !there || (none && !bad) ? -__builtin_inff() : bad ? nan : ln_p(given.v);
   }
   if (lane < a.top_k) {
     const bool is = key != 0 && !bad && !none;
@@ -458,7 +489,10 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(Logprobs
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
   const float c = factor_of(a.scale);
   Top top = {0, 0, kFloor<R>, 0, slots[id]};
+  Given<T> given;
+  if (splits == 1 && wave == 0) given.ask(a, t);
   Sums s = wave_part<T, TOP, W>(row, begin, end, wave, c, a.top_k, top);
+  if (splits == 1 && wave == 0) given.gather(a, t);
   if constexpr (W > 1) {
     if (lane == 0) sums[wave] = s;
     if (TOP && lane < a.top_k) keys[wave * a.top_k + lane] = static_cast<uint64_t>(top.hi) << 32 | top.lo;
@@ -466,11 +500,11 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void logprobs_kernel(Logprobs
     if (wave != 0) return;
     s = lane < W ? sums[lane < W ? lane : 0] : Sums{0.0, 0.0f, 0.0f};
     s = lanes_joined(s);
-    if constexpr (TOP) top = select_keys(keys, W * a.top_k, a.top_k, slots[0]);
+    if constexpr (TOP) top = select_keys(hold_keys(keys, W * a.top_k), keys, W * a.top_k, a.top_k, slots[0]);
   }
   const uint64_t key = static_cast<uint64_t>(top.hi) << 32 | top.lo;
   if (splits == 1) {
-    write_row<T>(a, t, s, key, c);
+    write_row<T>(a, t, s, key, c, given);
   } else {
     Sums* all = static_cast<Sums*>(a.workspace);
     if (lane == 0) all[part] = s;
@@ -486,17 +520,23 @@ __global__ __launch_bounds__(64) void join_kernel(LogprobsArgs a, int splits) {
   const int64_t t = blockIdx.x;
   const Sums* all = static_cast<const Sums*>(a.workspace);
   const uint64_t* keys = reinterpret_cast<const uint64_t*>(all + a.T * splits) + t * splits * a.top_k;
-  Sums s = {0.0, 0.0f, 0.0f};
-  for (int p0 = 0; p0 < splits; p0 += 64) {
-    const int p = p0 + static_cast<int>(threadIdx.x);
+  const int lane = threadIdx.x;
+  // everything is asked for before anything is waited for
+  Given<T> given;
+  given.ask(a, t);
+  Sums s = lane < splits ? all[t * splits + lane] : Sums{0.0, 0.0f, 0.0f};
+  const Held held = hold_keys(keys, splits * a.top_k);
+  __builtin_amdgcn_sched_barrier(0);
+  given.gather(a, t);
+  s = lanes_joined(s);
+  for (int p0 = 64; p0 < splits; p0 += 64) {
     Sums more = {0.0, 0.0f, 0.0f};
-    if (p < splits) more = all[t * splits + p];
-    more = lanes_joined(more);
-    s = p0 == 0 ? more : joined(s, more);
+    if (p0 + lane < splits) more = all[t * splits + p0 + lane];
+    s = joined(s, lanes_joined(more));
   }
   Top top = {};
-  if (a.top_k > 0) top = select_keys(keys, splits * a.top_k, a.top_k, slots);
-  write_row<T>(a, t, s, static_cast<uint64_t>(top.hi) << 32 | top.lo, factor_of(a.scale));
+  if (a.top_k > 0) top = select_keys(held, keys, splits * a.top_k, a.top_k, slots);
+  write_row<T>(a, t, s, static_cast<uint64_t>(top.hi) << 32 | top.lo, factor_of(a.scale), given);
 }
 
 // Rows that fill the card with a workgroup each; fewer are split.

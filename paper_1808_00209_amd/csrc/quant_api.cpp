@@ -67,8 +67,8 @@ bnn_status logprobs_check(const bnn_logprobs_desc* d) {
                 BNN_MAX_ALTERNATIVES);
   if (!real_type(d->dtype) && d->dtype != BNN_I32)
     return fail(BNN_ERR_SHAPE, "logprobs: unknown dtype %d", d->dtype);
-  if (!(d->logit_scale > 0.0f) || !isfinite(d->logit_scale))
-    return fail(BNN_ERR_SHAPE, "logprobs: logit_scale must be positive and finite");
+  if (!(d->logit_scale > 0.0f) || !(d->logit_scale <= 0x1p100f))
+    return fail(BNN_ERR_SHAPE, "logprobs: logit_scale must be positive and at most 2^100");
   return BNN_OK;
 }
 

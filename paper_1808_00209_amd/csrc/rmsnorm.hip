@@ -312,8 +312,23 @@ void launch_types(const NormArgs& a, hipStream_t s) {
   auto go = [&](auto wc, auto gc) {
     constexpr int W = decltype(wc)::value, G = decltype(gc)::value;
     constexpr int kRows = W > 4 ? 1 : 4 / W;
-    const unsigned grid = static_cast<unsigned>((a.M + kRows - 1) / kRows);
-    rmsnorm_kernel<T, TW, W, G><<<grid, W > 4 ? W * 64 : kNT, 0, s>>>(a);
+    // (a launch's work-items stay below 2^32: 2^21 workgroups of up to 1024)
+    constexpr int64_t kMost = int64_t{kRows} << 21;
+    for (int64_t m = 0; m < a.M; m += kMost) {
+      NormArgs b = a;
+      b.M = a.M - m < kMost ? a.M - m : kMost;
+      auto at = [&](const void* p, int64_t stride, size_t size) -> const void* {
+        return p ? static_cast<const char*>(p) + m * stride * static_cast<int64_t>(size) : nullptr;
+      };
+      b.x = at(a.x, a.x_stride, sizeof(T));
+      b.residual = at(a.residual, a.r_stride, sizeof(T));
+      b.sum = const_cast<void*>(at(a.sum, a.D, sizeof(T)));
+      b.y = const_cast<void*>(at(a.y, a.D, sizeof(T)));
+      b.q = a.q ? a.q + m * a.q_stride : nullptr;
+      b.scale = a.q ? a.scale + m : nullptr;
+      const unsigned grid = static_cast<unsigned>((b.M + kRows - 1) / kRows);
+      rmsnorm_kernel<T, TW, W, G><<<grid, W > 4 ? W * 64 : kNT, 0, s>>>(b);
+    }
   };
   const int groups = (a.D + 7) / 8;
   using std::integral_constant;

@@ -214,3 +214,28 @@ def test_far_rows():
     host = _logits(g, 3, V, "bf16")
     z.copy_(host)
     _check(host, torch.tensor([1, 2999, 5], dtype=torch.int32), 5, dev=z)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -120, 2.0 ** -30, 2.0 ** 30, 2.0 ** 100])
+def test_far_factors(scale):
+    """Factors that flatten a row, and that leave nothing but its largest."""
+    z = torch.tensor([[1.0, 2.0, 3.0, 3.0, -7.0], [0.0, 0.0, 0.0, 0.0, 0.0], [5.0, 5.0, -math.inf, 4.0, 1.0]])
+    z = z.repeat(1, 1000)
+    ids = torch.tensor([[2, 4], [1, 2], [2, 3]], dtype=torch.int32)
+    got = bnn.bnn_logprobs(z.cuda(), ids.cuda(), 3, scale)
+    given, entropy, top_ids, top = ref.logprobs(z, ids, 3, scale)
+    assert torch.equal(got[2].cpu(), top_ids)
+    _near(got[1], entropy, 2.0 ** -24 * 250 * 12)
+    _near(got[3], top, 2.0 ** -24 * 250)
+    want, lp = given.float().double(), got[0].cpu().double()  # (may pass fp32's range: -inf)
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(lp), fine)
+    assert ((lp - want).abs()[fine] <= 2.0 ** -24 * 250 + 2.0 ** -22 * want.abs()[fine]).all()
+
+
+@pytest.mark.parametrize("n", [64, 65, 1000])
+def test_many_given(n):
+    g = torch.Generator().manual_seed(16)
+    for T, V in ((2, 900), (1, 40000), (300, 6000)):
+        ids = torch.randint(-2, V + 2, (T, n), generator=g, dtype=torch.int32)
+        _check(_logits(g, T, V, "fp32"), ids, 2)

@@ -161,3 +161,22 @@ def test_single_outputs():
     assert torch.equal(full[2], only_q[2]) and torch.equal(full[3], only_q[3]) and only_q[1] is None
     empty = bnn.bnn_rmsnorm(x.cuda()[:0], w.cuda(), want_y=True)
     assert empty[1].shape == (0, 777) and empty[2].shape == (0, 777) and empty[3].shape == (0,)
+
+
+@pytest.mark.parametrize("D", [1, 520])
+def test_more_rows_than_a_launch_has(D):
+    """Rows past 2^21 workgroups (of four rows each, and of one)."""
+    M = (1 << 23) + 5 if D == 1 else (1 << 21) + 5
+    x = torch.ones(M, D, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(15)
+    ends = torch.cat([torch.arange(4), torch.arange(M - 9, M)])
+    rows = _rows(g, len(ends), D, "bf16")
+    x[ends.cuda()] = rows.cuda()
+    w = _rows(g, 1, D, "bf16")[0]
+    h, y, q, scale = bnn.bnn_rmsnorm(x, w.cuda(), x, want_y=True, sum=torch.empty_like(x))
+    hr, yr, qr, sr = ref.rmsnorm(rows, w, rows)
+    at = ends.cuda()
+    assert torch.equal(h[at].cpu(), hr) and torch.equal(q[at].cpu(), qr)
+    torch.testing.assert_close(scale[at].cpu().double(), sr, rtol=R, atol=0)
+    torch.testing.assert_close(y[at].cpu().double(), yr, rtol=R + 2.0 ** -8, atol=0)
+    assert (h[4:M - 9] == 2).all()

@@ -86,6 +86,7 @@ def _lp(lib, x=P, stride=30000, i=P, lp=P, e=P, ti=P, tl=P, ws=P, n_ws=1 << 40, 
     (dict(n=1025), "SHAPE", "n="), (dict(top_k=-1), "SHAPE", "top_k"), (dict(top_k=33), "SHAPE", "top_k"),
     (dict(V=4, top_k=5), "SHAPE", "top_k"), (dict(dtype=4), "SHAPE", "dtype"), (dict(dtype=-1), "SHAPE", "dtype"),
     (dict(logit_scale=0.0), "SHAPE", "logit_scale"), (dict(logit_scale=-1.0), "SHAPE", "logit_scale"),
+    (dict(logit_scale=2.0 ** 101), "SHAPE", "logit_scale"),
     (dict(logit_scale=float("nan")), "SHAPE", "logit_scale"), (dict(logit_scale=float("inf")), "SHAPE", "logit_scale"),
     (dict(stride=29999), "SHAPE", "stride"), (dict(stride=(1 << 31) + 1), "SHAPE", "stride"),
     (dict(x=None), "NULL", "logits"), (dict(i=None), "NULL", "ids"), (dict(lp=None), "NULL", "logp"),
