@@ -10,10 +10,21 @@
 //
 // The alternatives so far are a sorted list over the wave's lanes, one 64-bit
 // key each: the value's order in the high word, the inverted index in the low
-// one.  A group of 8 values per lane is looked at further only where its largest
+// one.  A step's 16 values per lane are looked at further only where the largest
 // reaches the top_k-th key, and values are inserted one by one; where many do
-// (the first group, rising rows), the bound is first raised to what top_k lanes'
-// largest values reach.
+// (the first step, rising rows), the bound is first raised to what top_k lanes'
+// largest values reach, and what still passes is placed by counting.
+//
+// 4096 x 131072 bf16, 8 alternatives: 194-211 us from card to card, 5.1 to 5.5
+// TB/s, a large copy's rate (without alternatives 200 where it took 210): bound
+// by memory.  16384 x 1000 int32, 5 alternatives: 23-25 us, 15 without: a wave
+// per row, 580 vector instructions of which the sums are 200, the vector ALU
+// three quarters busy.  301 x 50021 fp32, 8 alternatives: 22 us, 14 without: 1.2
+// rows per CU, of 16 waves that each fill a list (with 4 waves 24).  One row of
+// 65536: 12 us in two launches, chains of dependent steps.  Tried and dropped:
+// values through LDS instead of 16 copies of the insertion (T = 1: 16.2 us
+// against 14.4), the waves of a row sharing their bounds (16.1 against 13.5), the
+// next step's loads ahead (no gain).
 #include "dtypes.hpp"
 #include "quant.hpp"
 #include "wave_ops.hpp"
@@ -24,9 +35,9 @@ namespace bnn {
 namespace {
 
 constexpr int kNT = 256;  // unless a row has more waves
-constexpr int kEach = 16;           // values of a lane per step, in groups of 8
-constexpr int kStep = 64 * kEach;   // of a wave
-constexpr float kAway = 60.0f;
+constexpr int kEach = 16;          // values of a lane per step, in groups of 8
+constexpr int kStep = 64 * kEach;  // of a wave
+constexpr float kAway = 60.0f;     // a value this far above the reference moves it
 constexpr float kFar = 3e38f;    // the reference before there is one: minus this
 constexpr float kLarge = 0x1p20f; // the quick form's references, at most
 
@@ -539,9 +550,13 @@ __global__ __launch_bounds__(64) void join_kernel(LogprobsArgs a, int splits) {
   write_row<T>(a, t, s, static_cast<uint64_t>(top.hi) << 32 | top.lo, factor_of(a.scale), given);
 }
 
-// Rows that fill the card with a workgroup each; fewer are split.
+// From kFull rows on, each is one workgroup's (or wave's): 1024 x 32768 25 us, in
+// parts and joined 33.  Fewer are split into parts of 4 steps or more per wave
+// (one row of 65536: 12.2 us; as one workgroup of 16 waves 22, in parts of a
+// quarter each 14).  Long rows that leave CUs with one or two workgroups go to 16
+// waves (301 x 50021: 22 us, 4 waves 24).
 constexpr int kFull = 256;
-constexpr int kParts = 1024;       // parts that fill it
+constexpr int kParts = 1024;        // parts that fill the card
 constexpr int kLength = 4 * kStep;  // a part's values, at least
 
 int64_t most_splits(int32_t V) { return (V + kLength - 1) / kLength; }

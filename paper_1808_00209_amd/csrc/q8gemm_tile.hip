@@ -1,17 +1,27 @@
 // 8-bit matrix product of many rows whose operands lie on 16-byte steps
 // (bnn_q8gemm) on the int8 matrix cores.
 //
-// A workgroup of 2 x 2 waves computes 64 TM rows x 64 TN outputs, a wave 32 TM x
-// 32 TN.  128 bytes of every row of both operands (a stage) go from memory
-// straight into LDS, S stages in turn: while one is multiplied the next ones are
-// on their way.  A wave reads the operands of its next matrix instructions while
-// the present ones run, also over the stages' ends: the wait and the barrier
-// come before a stage's last products.
+// A workgroup of WM x WN waves computes 32 TM WM rows x 32 TN WN outputs, a wave
+// 32 TM x 32 TN.  128 bytes of every row of both operands (a stage) go from
+// memory straight into LDS, S stages in turn: while one is multiplied the next
+// ones are on their way.  A wave reads the operands of its next matrix
+// instructions while the present ones run, also over the stages' ends: the wait
+// and the barrier come before a stage's last products.
 //
 // LDS is filled in the order of the lanes, so rows are 128 bytes apart there;
 // a row's eight 16-byte chunks are stored in an order of its own (chunk j at
 // j ^ (row / 2 % 8), by the address each lane loads from), so that a wave's
 // reads of one chunk from 32 rows spread over the banks.
+//
+// 8192 x 16384 outputs, K 4096, bf16 out: 488-509 us from card to card, 2.16 to
+// 2.25e15 operations a second, what a large library product of these bytes
+// reaches here (2.24e15); the card's clock is at 1.7 GHz then, the matrix cores
+// busy in 60 % of the cycles.  Tried there: four waves of 128 x 128 (half the
+// LDS reads; 488 us against 490), bands of 2 to 16 row tiles (497-506).  Outputs
+// stored by each lane as they came took 640 us: through LDS they leave in runs.
+// 256 x 4096 outputs, K 4096 (a tile of 64 per CU): 9.9 us, of which the 32
+// stages' loads and barriers are about 6 (their wait counted, so that two later
+// stages stay on their way: 17.8 us without; K split over the waves: 10.6).
 #include "q8gemm.hpp"
 
 namespace bnn {
@@ -29,8 +39,8 @@ typedef const __attribute__((address_space(1))) void global_void;
 __device__ const v4i q8_zeros[1] = {{0, 0, 0, 0}};
 
 template <class T, int TM, int TN, int WM, int WN, int S>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4 * (TM * TN < 8 ? 2 : 1)) void q8_tile_kernel(Q8Args a, int cols, int tiles,
-                                                                             int per_xcd, int band) {
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4 * (TM * TN < 8 ? 2 : 1)) void q8_tile_kernel(
+    Q8Args a, int cols, int tiles, int per_xcd, int band) {
   constexpr int kNT = 64 * WM * WN;
   constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN, kRows = BM + BN;
   constexpr int kLoads = kRows * kChunks / kNT;  // of a thread, per stage
@@ -280,16 +290,12 @@ void launch_shape(const Q8Args& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_q8_tile(const Q8Args& a, Q8Form form, hipStream_t s) {
-#ifdef Q8_FORCE
-  launch_shape<Q8_FORCE>(a, s);
-#else
   switch (form) {
     case kQ8Tile256: launch_shape<4, 2, 2, 4, 2>(a, s); break;
     case kQ8Pair128: launch_shape<2, 2, 2, 2, 2>(a, s); break;
     case kQ8Tile128: launch_shape<2, 1, 2, 4, 4>(a, s); break;
     default: launch_shape<1, 1, 2, 2, 4>(a, s); break;
   }
-#endif
   return hipGetLastError();
 }
 
