@@ -17,7 +17,7 @@
 //
 // 4096 x 131072 bf16, 8 alternatives: 194-211 us from card to card, 5.1 to 5.5
 // TB/s, a large copy's rate (without alternatives 200 where it took 210): bound
-// by memory.  16384 x 1000 int32, 5 alternatives: 23-25 us, 15 without: a wave
+// by memory.  16384 x 1000 int32, 5 alternatives: 23-25 us, 14 without: a wave
 // per row, 580 vector instructions of which the sums are 200, the vector ALU
 // three quarters busy.  301 x 50021 fp32, 8 alternatives: 22 us, 14 without: 1.2
 // rows per CU, of 16 waves that each fill a list (with 4 waves 24).  One row of
@@ -150,14 +150,15 @@ struct Top {
 };
 
 // Raises top.floor to an order that the values of at least top_k lanes reach
-// (mine: a lane's largest, 0 for none): ten bits of it below those that all
-// lanes' have in common, a lower bound of the top_k-th being all that is asked.
+// (mine: a lane's largest, 0 for none): 14 bits of it below those that all lanes'
+// have in common, a lower bound of the top_k-th being all that is asked (6 bits
+// let too many through: 301 x 50021 34 us instead of 22).
 __device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) {
   const uint32_t most = wave_max(mine), least = wave_min(mine ? mine : ~0u);
   const int own = most == least ? 0 : 32 - __builtin_clz(most ^ least);  // bits
   uint32_t at = own < 32 ? most >> own << own : 0;
   if (__popcll(__ballot(mine >= at && mine != 0)) < top_k) return;
-  for (int b = own - 1; b >= 0 && b >= own - 10; --b) {
+  for (int b = own - 1; b >= 0 && b >= own - 14; --b) {
     const uint32_t next = at | 1u << b;
     if (__popcll(__ballot(mine >= next)) >= top_k) at = next;
   }
@@ -180,9 +181,8 @@ struct Scan {
     if constexpr (SAFE) return v == -__builtin_inff() ? v : (v - ref) * c;
     else return __builtin_fmaf(v, c, -ref);
   }
-  // FINITE: no value is -inf.
-  template <bool FINITE>
-  __device__ __forceinline__ void add(const float (&v)[kEach], float fm) {
+  // The reference for values up to fm (of each lane).
+  __device__ __forceinline__ void refer(float fm) {
     if (__any(SAFE ? fm > ref : delta(fm) > kAway)) {
       const float top = wave_max(fm);
       const float next = SAFE ? top : top * c;
@@ -195,21 +195,22 @@ struct Scan {
       s1 *= f;
       ref = next;
     }
+  }
+  // FINITE: no value is -inf.
+  template <bool FINITE>
+  __device__ __forceinline__ void add(const float (&v)[8]) {
+    float e[8], d[8];
 #pragma unroll
-    for (int g = 0; g < kEach; g += 8) {
-      float e[8], d[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        d[i] = delta(v[g + i]);
-        e[i] = exp2_of(d[i]);
-        if (!FINITE) d[i] = __builtin_fmaxf(d[i], -200.0f);  // (0 * -inf)
-      }
-      s1 += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-      float t = e[0] * d[0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) t = __builtin_fmaf(e[i], d[i], t);
-      s2 += t;
+    for (int i = 0; i < 8; ++i) {
+      d[i] = delta(v[i]);
+      e[i] = exp2_of(d[i]);
+      if (!FINITE) d[i] = __builtin_fmaxf(d[i], -200.0f);  // (0 * -inf)
     }
+    s1 += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+    float t = e[0] * d[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t = __builtin_fmaf(e[i], d[i], t);
+    s2 += t;
   }
   __device__ __forceinline__ Sums total() const {
     return {SAFE ? static_cast<double>(ref) * c : static_cast<double>(ref), wave_sum(s1),
@@ -241,25 +242,33 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
   sc.start(c);
   // A step: group g of a lane's 8 values starts at index at + 512 g + 8 lane.
   // What lies past the row's end is -inf; integers have no such value, so there
-  // `n` says how many of each group are in the row (part: of some lane, not 8).
+  // `n` says how many of each group are in the row: all (kAll), all or none
+  // (kWhole), or some (kSome).
+  constexpr int kAll = 0, kWhole = 1, kSome = 2;
   auto step = [&](const R (&v)[kEach], int at, const int (&n)[kGroups], auto part) {
-    constexpr bool kPart = kInts && decltype(part)::value;
-    float f[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      f[i] = static_cast<float>(v[i]);
-      if (kPart) f[i] = i % 8 < n[i / 8] ? f[i] : -__builtin_inff();
-    }
+    constexpr int kPart = kInts ? decltype(part)::value : kAll;
+    auto in = [&](int i) { return kPart == kAll || (kPart == kWhole ? n[i / 8] > 0 : i % 8 < n[i / 8]); };
     R m = v[0];
-    if constexpr (kInts) {  // (beyond 2^24 their order is not that of f)
+    if constexpr (kInts) {  // (beyond 2^24 their order is not that of fp32)
 #pragma unroll
       for (int i = 1; i < kEach; ++i) m = m > v[i] ? m : v[i];
     } else {
 #pragma unroll
       for (int i = 1; i < kEach; ++i) m = __builtin_fmaxf(m, v[i]);
     }
-    const bool some = !kPart || n[0] > 0;  // (past the end: the least integer)
-    sc.template add<kInts && !kPart>(f, some ? static_cast<float>(m) : -__builtin_inff());
+    const bool some = kPart == kAll || n[0] > 0;  // (past the end: the least integer)
+    sc.refer(some ? static_cast<float>(m) : -__builtin_inff());
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      if (kPart == kWhole && n[g] <= 0) continue;
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        f[i] = static_cast<float>(v[8 * g + i]);
+        if (kPart == kSome) f[i] = i < n[g] ? f[i] : -__builtin_inff();
+      }
+      sc.template add<kInts && kPart != kSome>(f);
+    }
     if constexpr (TOP) {
       const uint32_t mo = some ? order_of(m) : 0u;
       const uint64_t reach = __ballot(some && mo >= top.floor);
@@ -267,9 +276,11 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
         if (__popcll(reach) > 12) raise_floor(top, mo, top_k);
         R floor;
         value_of(top.floor, floor);
-        auto passes = [&](int i) { return v[i] >= floor && (!kPart || i % 8 < n[i / 8]); };
+        auto passes = [&](int i) { return v[i] >= floor && in(i); };
         auto index_of = [&](int i, int l) { return static_cast<uint32_t>(at + i / 8 * 512 + 8 * l + i % 8); };
-        if (top.bound == 0) {  // (the list is not full: most often, empty)
+        // (an empty list of few is filled sooner by inserting: 16384 x 1000, 5
+        // alternatives 23.4 us : 25.6; 301 x 50021, 8 alternatives 27 : 22)
+        if (top_k > 6 && top.bound == 0) {  // (not full: most often, empty)
           const bool empty = __builtin_amdgcn_readlane(top.hi | top.lo, 0) == 0;
           int count = 0;
           if (empty) {
@@ -316,7 +327,7 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) e[g] = load8(row + at + 512 * g + 8 * lane);
     take(e);
-    step(v, at, n, std::false_type{});
+    step(v, at, n, std::integral_constant<int, kAll>{});
   }
   if (at < end) {
     Eight<T> e[kGroups];
@@ -335,7 +346,8 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
       }
     }
     take(e);
-    step(v, at, n, std::true_type{});
+    if (kInts && (end - at) % 8 == 0) step(v, at, n, std::integral_constant<int, kWhole>{});
+    else step(v, at, n, std::integral_constant<int, kSome>{});
   }
   return sc.total();
 }

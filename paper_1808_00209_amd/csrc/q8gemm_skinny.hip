@@ -6,8 +6,9 @@
 // tiles, the next one's weights in flight while the present one's sums are
 // added up over the KW waves in LDS.
 //
-// Bound by the weights: 65536 outputs, K 4096 in 59.8 us, 4.5 TB/s (a large copy
-// reaches 5.1); 4096 outputs, one row: 7.5 us, of which the weights take 3.3.
+// Bound by the weights: 65536 outputs, K 4096: one row in 53.1 us, 5.05 TB/s (a
+// large copy reaches 5.1), 16 rows in 58.0, 4.6 TB/s; 4096 outputs, one row: 7.3
+// us, of which the weights take 3.3.
 #include "dtypes.hpp"
 #include "q8gemm.hpp"
 
@@ -32,6 +33,17 @@ __global__ __launch_bounds__(kNT) void q8_skinny_kernel(Q8Args a, int kw_log, in
   // loaded, and x's that belong to other chunks (or to none) are zeroed.
   auto chunk_at = [&](int s) { return min((first + s) * kStep + 16 * g, a.K - 16); };
 
+  const int tiles = (a.N + 15) / 16;
+  v4i w[P];
+  auto load_w = [&](int tile) {
+    const int8_t* row =
+        a.w + static_cast<int64_t>(min(16 * tile + r, a.N - 1)) * a.w_stride;
+#pragma unroll
+    for (int s = 0; s < P; ++s)
+      if (s < steps) w[s] = *reinterpret_cast<const v4i_any*>(row + chunk_at(s));
+  };
+  load_w(blockIdx.x * NW + wn);  // (on their way before x's)
+  __builtin_amdgcn_sched_barrier(0);
   v4i x[MT][P];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
@@ -47,19 +59,9 @@ __global__ __launch_bounds__(kNT) void q8_skinny_kernel(Q8Args a, int kw_log, in
     }
   }
 
-  const int tiles = (a.N + 15) / 16;
-  v4i w[P];
-  auto load_w = [&](int tile) {
-    const int8_t* row =
-        a.w + static_cast<int64_t>(min(16 * tile + r, a.N - 1)) * a.w_stride;
-#pragma unroll
-    for (int s = 0; s < P; ++s)
-      if (s < steps) w[s] = *reinterpret_cast<const v4i_any*>(row + chunk_at(s));
-  };
   T* y = static_cast<T*>(a.y);
   int buf = 0;
   const int jump = gridDim.x * NW;
-  load_w(blockIdx.x * NW + wn);
   for (int tile0 = blockIdx.x * NW; tile0 < tiles; tile0 += jump, buf ^= 1) {
     v4i acc[MT] = {};
 #pragma unroll
@@ -117,7 +119,7 @@ hipError_t launch_q8_skinny(const Q8Args& a, hipStream_t s) {
   const int steps = (all + (1 << kw_log) - 1) >> kw_log;
   const int tiles = (a.N + 15) / 16;
   const int sets = (tiles + (kWaves >> kw_log) - 1) / (kWaves >> kw_log);
-  // Two workgroups per CU (16 x 65536 outputs, K 4096: 59.8 us, one per CU 60.7);
+  // Two workgroups per CU (16 x 65536 outputs, K 4096: 58.0 us, one per CU 61.3);
   // with more rows, whose x each of them reads, one (64 x 16384: 25.0 us, two 36.2).
   const int most = a.M <= 16 ? 512 : 256;
   const int grid = sets < most ? sets : most;
