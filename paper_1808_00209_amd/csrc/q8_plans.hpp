@@ -27,11 +27,11 @@ inline int64_t q8_tiles(int64_t M, int64_t N, int n) { return (M + n - 1) / n * 
 // 46, the clock being higher).  Other K move all of them alike.
 //
 // Few rows (us, skinny : tiles of 64, K 4096): 16 rows of 4096 outputs 8.0 : 8.7
-// and of 65536 59.7 : 59.4, 32 rows 10.6 : 8.9 and 19.7 : 13.6 (16384 outputs),
-// 64 rows 15.9 : 9.4.  Above 16 the tiles' rows are shared by a workgroup's waves.
+// and of 65536 58.0 : 59.4; 32 rows, in two operands of the skinny kernel, 10.6 :
+// 8.9 and 19.7 : 13.6 (16384 outputs): there a workgroup's waves share the rows.
+// x stays in the skinny kernel's registers up to K 8192.
 inline Q8Form q8_form(int64_t M, int64_t N, int64_t K, bool on16) {
-  const bool short_k = (M <= 32 && K <= 8192) || (M <= 64 && K <= 4096);  // x fits the registers
-  if (K >= 16 && short_k && (M <= 16 || !on16)) return kQ8Skinny;
+  if (K >= 16 && K <= 8192 && M <= 16) return kQ8Skinny;
   if (K < 16 || !on16) return kQ8Any;
   const int64_t t64 = q8_tiles(M, N, 64), t128 = q8_tiles(M, N, 128), t256 = q8_tiles(M, N, 256);
   const int64_t in64 = 3 + 7 * t64 / 256;

@@ -1,9 +1,11 @@
 // Matrix product of 8-bit integers with a scale per row and per output
 // (bnn_q8gemm): the choice of kernel, and the one for operands that lie anywhere
-// (rows that are not on 16-byte steps, K below 16).  Its 128 x 128 tiles are
-// staged through registers, where K's end is masked, one stage at a time: 256 x
-// 4096 outputs, K 4096 in 129 us where the tiles of q8gemm_tile.hip take 9.9, so
-// that rows worth a second look are worth laying out 16 bytes apart.
+// (rows that are not on 16-byte steps, K below 16).  Its tiles go through
+// registers into two LDS buffers in turn: unaligned 16-byte loads, K's end masked
+// on the way, the next stage's on their way while one is multiplied.
+// 256 x 4096 outputs, K 4095: 30 us, 8192 x 16384 1205 (the tiles of
+// q8gemm_tile.hip, K 4096: 9.9 and 500; one buffer and no load ahead 133 and
+// 1290): weights that are used often are worth laying out 16 bytes apart.
 #include "q8gemm.hpp"
 
 namespace bnn {
@@ -38,51 +40,63 @@ __device__ __forceinline__ v4i load16(const int8_t* row, int k, int K) {
 // A workgroup of 2 x 2 waves, 64 TM rows x 64 TN outputs.
 template <class T, int TM, int TN>
 __global__ __launch_bounds__(kNT) void q8_any_kernel(Q8Args a) {
-  extern __shared__ v4i lds[];
   constexpr int BM = 64 * TM, BN = 64 * TN;
+  constexpr int kLoads = (BM + BN) * kChunks / kNT;
+  __shared__ v4i lds[2][(BM + BN) * kChunks];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = lane >> 5, c = lane & 31;
   const unsigned cols = (a.N + BN - 1) / BN;
   const int64_t m0 = static_cast<int64_t>(blockIdx.x / cols) * BM;
   const int n0 = static_cast<int>(blockIdx.x % cols) * BN;
-  v4i* lx = lds;
-  v4i* lw = lds + BM * kChunks;
-  v16i acc[TM][TN] = {};
-  const int wm = (wave >> 1) * 32 * TM, wn = (wave & 1) * 32 * TN;
-  for (int k0 = 0; k0 < a.K; k0 += kBK) {
-    for (int i = tid; i < (BM + BN) * kChunks; i += kNT) {
-      const int row = i / kChunks, j = i % kChunks;
-      const int8_t* p;
-      if (row < BM) p = a.x + min(m0 + row, a.M - 1) * a.x_stride;
-      else p = a.w + static_cast<int64_t>(min(n0 + row - BM, a.N - 1)) * a.w_stride;
-      lds[row * kChunks + (j ^ (row & 7))] = load16(p, k0 + 16 * j, a.K);
+  const int j = tid % kChunks;  // the thread's chunk of its rows
+  const int8_t* rows[kLoads];
+#pragma unroll
+  for (int l = 0; l < kLoads; ++l) {
+    const int row = (l * kNT + tid) / kChunks;
+    rows[l] = row < BM ? a.x + min(m0 + row, a.M - 1) * a.x_stride
+                       : a.w + static_cast<int64_t>(min(n0 + row - BM, a.N - 1)) * a.w_stride;
+  }
+  v4i next[kLoads];
+  auto load = [&](int k0) {
+    if (k0 + kBK <= a.K) {
+#pragma unroll
+      for (int l = 0; l < kLoads; ++l)
+        next[l] = *reinterpret_cast<const v4i_any*>(rows[l] + k0 + 16 * j);
+    } else {
+#pragma unroll
+      for (int l = 0; l < kLoads; ++l) next[l] = load16(rows[l], k0 + 16 * j, a.K);
     }
-    __syncthreads();
+  };
+  v16i acc[TM][TN] = {};
+  const int wm = (wave >> 1) * 32 * TM, wn = BM + (wave & 1) * 32 * TN;
+  load(0);
+  for (int k0 = 0, buf = 0; k0 < a.K; k0 += kBK, buf ^= 1) {
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      const int row = (l * kNT + tid) / kChunks;
+      lds[buf][row * kChunks + (j ^ (row & 7))] = next[l];
+    }
+    __syncthreads();  // (the other buffer's readers are past the barrier before)
+    if (k0 + kBK < a.K) load(k0 + kBK);
+    auto chunk = [&](int row, int s) { return lds[buf][row * kChunks + ((2 * s + h) ^ (row & 7))]; };
 #pragma unroll
     for (int s = 0; s < kBK / 32; ++s) {
       v4i x[TM], w[TN];
 #pragma unroll
-      for (int t = 0; t < TM; ++t) {
-        const int row = wm + 32 * t + c;
-        x[t] = lx[row * kChunks + ((2 * s + h) ^ (row & 7))];
-      }
+      for (int t = 0; t < TM; ++t) x[t] = chunk(wm + 32 * t + c, s);
 #pragma unroll
-      for (int t = 0; t < TN; ++t) {
-        const int row = wn + 32 * t + c;
-        w[t] = lw[row * kChunks + ((2 * s + h) ^ (row & 7))];
-      }
+      for (int t = 0; t < TN; ++t) w[t] = chunk(wn + 32 * t + c, s);
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[i], w[j], acc[i][j], 0, 0, 0);
+        for (int k = 0; k < TN; ++k)
+          acc[i][k] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[i], w[k], acc[i][k], 0, 0, 0);
     }
-    __syncthreads();
   }
   T* y = static_cast<T*>(a.y);
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int n = n0 + wn + 32 * j + c;
+  for (int k = 0; k < TN; ++k) {
+    const int n = n0 + wn - BM + 32 * k + c;
     const int nc = min(n, a.N - 1);
     const float ws = a.w_scale ? a.w_scale[nc] : 1.0f;
     const float bias = a.bias ? a.bias[nc] : 0.0f;
@@ -93,7 +107,7 @@ __global__ __launch_bounds__(kNT) void q8_any_kernel(Q8Args a) {
         const int64_t m = m0 + wm + 32 * i + 8 * (e / 4) + 4 * h + e % 4;
         if (m < a.M && n < a.N) {
           const float xs = a.x_scale ? a.x_scale[m] : 1.0f;
-          y[m * a.N + n] = from_f32<T>(static_cast<float>(acc[i][j][e]) * xs * ws + bias);
+          y[m * a.N + n] = q8_output<T>(acc[i][k][e], xs, ws, bias);
         }
       }
   }
@@ -108,13 +122,16 @@ hipError_t launch_q8gemm(const Q8Args& a, hipStream_t s) {
   const Q8Form form = q8_form(a.M, a.N, a.K, on16(a.x, a.x_stride) && on16(a.w, a.w_stride));
   if (form == kQ8Skinny) return launch_q8_skinny(a, s);
   if (form != kQ8Any) return launch_q8_tile(a, form, s);
-  constexpr int TM = 2, TN = 2;
-  const int64_t cols = (a.N + 64 * TN - 1) / (64 * TN), rows = (a.M + 64 * TM - 1) / (64 * TM);
-  const unsigned grid = static_cast<unsigned>(rows * cols);  // M * N <= 2^35: below 2^23 + 2^18
-  with_real_type(a.dtype, [&](auto t) {
-    using T = decltype(t);
-    q8_any_kernel<T, TM, TN><<<grid, kNT, size_t{64} * (TM + TN) * kBK, s>>>(a);
-  });
+  auto any = [&](auto size) {
+    constexpr int TS = decltype(size)::value;
+    const int64_t tiles = q8_tiles(a.M, a.N, 64 * TS);  // M * N <= 2^35: below 2^24
+    with_real_type(a.dtype, [&](auto t) {
+      q8_any_kernel<decltype(t), TS, TS><<<static_cast<unsigned>(tiles), kNT, 0, s>>>(a);
+    });
+  };
+  // (tiles of 64 where those of 128 leave CUs without one)
+  if (q8_tiles(a.M, a.N, 128) >= 256) any(std::integral_constant<int, 2>{});
+  else any(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
 

@@ -1,4 +1,4 @@
-// 8-bit matrix product of few rows (bnn_q8gemm, up to 64 rows): every weight is
+// 8-bit matrix product of few rows (bnn_q8gemm, up to 16 rows): every weight is
 // read once, straight into the int8 matrix cores' registers.
 //
 // A workgroup's 8 waves split K among KW of them (a wave's share of x stays in
@@ -19,10 +19,10 @@ constexpr int kWaves = 8;
 constexpr int kNT = 64 * kWaves;
 constexpr int kStep = 64;  // bytes of K per matrix instruction
 
-// MT: 16-row tiles of x.  P: a wave's steps along K, at most.
-template <class T, int MT, int P>
+// P: a wave's steps along K, at most.
+template <class T, int P>
 __global__ __launch_bounds__(kNT) void q8_skinny_kernel(Q8Args a, int kw_log, int steps) {
-  __shared__ v4i part[2][kWaves][MT][64];
+  __shared__ v4i part[2][kWaves][64];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
@@ -44,58 +44,51 @@ __global__ __launch_bounds__(kNT) void q8_skinny_kernel(Q8Args a, int kw_log, in
   };
   load_w(blockIdx.x * NW + wn);  // (on their way before x's)
   __builtin_amdgcn_sched_barrier(0);
-  v4i x[MT][P];
+  v4i x[P];
+  const int8_t* row = a.x + min(static_cast<int64_t>(r), a.M - 1) * a.x_stride;
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int8_t* row = a.x + min(static_cast<int64_t>(16 * t + r), a.M - 1) * a.x_stride;
-#pragma unroll
-    for (int s = 0; s < P; ++s) {
-      v4i v = {0, 0, 0, 0};
-      if (s < steps) {
-        const int k = (first + s) * kStep + 16 * g;
-        v = low_bytes_cleared(*reinterpret_cast<const v4i_any*>(row + chunk_at(s)), k - chunk_at(s));
-      }
-      x[t][s] = v;
+  for (int s = 0; s < P; ++s) {
+    v4i v = {0, 0, 0, 0};
+    if (s < steps) {
+      const int k = (first + s) * kStep + 16 * g;
+      v = low_bytes_cleared(*reinterpret_cast<const v4i_any*>(row + chunk_at(s)), k - chunk_at(s));
     }
+    x[s] = v;
   }
-
   T* y = static_cast<T*>(a.y);
+  const float xs = a.x_scale ? a.x_scale[min(static_cast<int64_t>(r), a.M - 1)] : 1.0f;
   int buf = 0;
   const int jump = gridDim.x * NW;
   for (int tile0 = blockIdx.x * NW; tile0 < tiles; tile0 += jump, buf ^= 1) {
-    v4i acc[MT] = {};
+    // the factors of the outputs that this wave will write, asked for early
+    const int n = 16 * (tile0 + wave) + 4 * g;
+    float ws[4], bias[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int nc = min(n + e, a.N - 1);
+      ws[e] = wave < NW && a.w_scale ? a.w_scale[nc] : 1.0f;
+      bias[e] = wave < NW && a.bias ? a.bias[nc] : 0.0f;
+    }
+    v4i acc = {0, 0, 0, 0};
 #pragma unroll
     for (int s = 0; s < P; ++s)
-      if (s < steps) {
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s], x[t][s], acc[t], 0, 0, 0);
-      }
+      if (s < steps) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s], x[s], acc, 0, 0, 0);
     if (tile0 + jump < tiles) load_w(tile0 + jump + wn);
-#pragma unroll
-    for (int t = 0; t < MT; ++t) part[buf][wave][t][lane] = acc[t];
+    part[buf][wave][lane] = acc;
     __syncthreads();
-    // NW x MT tiles of 16 outputs x 16 rows; lane (g, r) has outputs 4 g .. of
-    // row r.
-    for (int i = wave; i < NW * MT; i += kWaves) {
-      const int n_tile = i / MT, t = i % MT;
-      v4i sum = part[buf][n_tile << kw_log][t][lane];
+    // NW tiles of 16 outputs x 16 rows; lane (g, r) has outputs 4 g .. of row r.
+    if (wave < NW) {
+      v4i sum = part[buf][wave << kw_log][lane];
       for (int k = 1; k < KW; ++k) {
-        const v4i p = part[buf][(n_tile << kw_log) + k][t][lane];
+        const v4i p = part[buf][(wave << kw_log) + k][lane];
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += p[e];
       }
-      const int m = 16 * t + r, n = 16 * (tile0 + n_tile) + 4 * g;
-      if (m < a.M && n < a.N) {
-        const float xs = a.x_scale ? a.x_scale[m] : 1.0f;
+      if (r < a.M && n < a.N) {
         T out[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int nc = min(n + e, a.N - 1);
-          out[e] = q8_output<T>(sum[e], xs, a.w_scale ? a.w_scale[nc] : 1.0f,
-                                a.bias ? a.bias[nc] : 0.0f);
-        }
-        T* at = y + static_cast<int64_t>(m) * a.N + n;
+        for (int e = 0; e < 4; ++e) out[e] = q8_output<T>(sum[e], xs, ws[e], bias[e]);
+        T* at = y + static_cast<int64_t>(r) * a.N + n;
         if (a.N % 4 == 0) {
           typedef uint32_t out_words __attribute__((ext_vector_type(sizeof(T)), aligned(8)));
           out_words v;
@@ -119,25 +112,13 @@ hipError_t launch_q8_skinny(const Q8Args& a, hipStream_t s) {
   const int steps = (all + (1 << kw_log) - 1) >> kw_log;
   const int tiles = (a.N + 15) / 16;
   const int sets = (tiles + (kWaves >> kw_log) - 1) / (kWaves >> kw_log);
-  // Two workgroups per CU (16 x 65536 outputs, K 4096: 58.0 us, one per CU 61.3);
-  // with more rows, whose x each of them reads, one (64 x 16384: 25.0 us, two 36.2).
-  const int most = a.M <= 16 ? 512 : 256;
-  const int grid = sets < most ? sets : most;
+  // two workgroups per CU (16 x 65536 outputs, K 4096: 58.0 us, one per CU 61.3)
+  const int grid = sets < 512 ? sets : 512;
   with_real_type(a.dtype, [&](auto t) {
     using T = decltype(t);
-    auto go = [&](auto mc, auto pc) {
-      q8_skinny_kernel<T, decltype(mc)::value, decltype(pc)::value>
-          <<<grid, kNT, 0, s>>>(a, kw_log, steps);
-    };
-    using std::integral_constant;
-    auto rows = [&](auto pc) {
-      if (a.M <= 16) return go(integral_constant<int, 1>{}, pc);
-      if (a.M <= 32) return go(integral_constant<int, 2>{}, pc);
-      if constexpr (decltype(pc)::value <= 8) go(integral_constant<int, 4>{}, pc);
-    };
-    if (steps <= 4) rows(integral_constant<int, 4>{});
-    else if (steps <= 8) rows(integral_constant<int, 8>{});
-    else rows(integral_constant<int, 16>{});
+    if (steps <= 4) q8_skinny_kernel<T, 4><<<grid, kNT, 0, s>>>(a, kw_log, steps);
+    else if (steps <= 8) q8_skinny_kernel<T, 8><<<grid, kNT, 0, s>>>(a, kw_log, steps);
+    else q8_skinny_kernel<T, 16><<<grid, kNT, 0, s>>>(a, kw_log, steps);
   });
   return hipGetLastError();
 }

@@ -49,8 +49,8 @@ def test_forms_fit_their_sizes():
             for K in (1, 15, 16, 4096, 4097, 8192, 8193, 131071):
                 for on16 in (False, True):
                     f = _form(M, N, K, on16)
-                    if f == SKINNY:  # x in registers: 4 tiles of 8 steps or 2 of 16
-                        assert K >= 16 and (M <= 32 and K <= 8192 or M <= 64 and K <= 4096)
+                    if f == SKINNY:  # x in registers: 16 steps of 64 per wave
+                        assert 16 <= K <= 8192 and M <= 16
                     elif f != ANY:
                         assert K >= 16 and on16
                     else:
