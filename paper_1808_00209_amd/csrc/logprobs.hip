@@ -105,6 +105,13 @@ struct Top {
     if (bh > floor) floor = bh;
   }
 
+  // Whether a key (uniform) is beyond the bound, in 32-bit steps that the scalar
+  // unit has.
+  __device__ __forceinline__ bool beyond(uint32_t order, uint32_t low) const {
+    const uint32_t bh = static_cast<uint32_t>(bound >> 32);
+    return order > bh || (order == bh && low > static_cast<uint32_t>(bound));
+  }
+
   // A key of the lanes where `is` holds, put behind the `count` ones in slots
   // (past 64: only counted).
   __device__ __forceinline__ void collect(uint64_t key, bool is, int& count) {
@@ -154,7 +161,9 @@ struct Top {
 // have in common, a lower bound of the top_k-th being all that is asked (6 bits
 // let too many through: 301 x 50021 34 us instead of 22).
 __device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) {
-  const uint32_t most = wave_max(mine), least = wave_min(mine ? mine : ~0u);
+  // (known as uniform: what follows is the scalar unit's)
+  const uint32_t most = __builtin_amdgcn_readfirstlane(wave_max(mine));
+  const uint32_t least = __builtin_amdgcn_readfirstlane(wave_min(mine ? mine : ~0u));
   const int own = most == least ? 0 : 32 - __builtin_clz(most ^ least);  // bits
   uint32_t at = own < 32 ? most >> own << own : 0;
   if (__popcll(__ballot(mine >= at && mine != 0)) < top_k) return;
@@ -302,9 +311,9 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
             mask &= mask - 1;
             const uint32_t o = order_of(__builtin_bit_cast(
                 R, __builtin_amdgcn_readlane(__builtin_bit_cast(uint32_t, v[i]), l)));
-            const uint64_t key = static_cast<uint64_t>(o) << 32 | static_cast<uint32_t>(~index_of(i, l));
-            if (key > top.bound) {
-              top.insert(key, top_k);
+            const uint32_t low = ~index_of(i, l);
+            if (top.beyond(o, low)) {
+              top.insert(static_cast<uint64_t>(o) << 32 | low, top_k);
               value_of(top.floor, floor);
             }
           }
@@ -413,9 +422,8 @@ __device__ __forceinline__ Top select_keys(const Held& h, const uint64_t* keys, 
     while (mask) {
       const int l = __builtin_ctzll(mask);
       mask &= mask - 1;
-      const uint64_t k = static_cast<uint64_t>(__builtin_amdgcn_readlane(hi, l)) << 32 |
-                         static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, l));
-      if (k > top.bound) top.insert(k, top_k);
+      const uint32_t o = __builtin_amdgcn_readlane(hi, l), low = __builtin_amdgcn_readlane(lo, l);
+      if (top.beyond(o, low)) top.insert(static_cast<uint64_t>(o) << 32 | low, top_k);
     }
   }
   return top;
