@@ -15,16 +15,16 @@
 // (the first step, rising rows), the bound is first raised to what top_k lanes'
 // largest values reach, and what still passes is placed by counting.
 //
-// 4096 x 131072 bf16, 8 alternatives: 194-211 us from card to card, 5.1 to 5.5
+// 4096 x 131072 bf16, 8 alternatives: 193-210 us from card to card, 5.1 to 5.5
 // TB/s, a large copy's rate (without alternatives 200 where it took 210): bound
-// by memory.  16384 x 1000 int32, 5 alternatives: 23-25 us, 14 without: a wave
-// per row, 580 vector instructions of which the sums are 200, the vector ALU
-// three quarters busy.  301 x 50021 fp32, 8 alternatives: 22 us, 14 without: 1.2
-// rows per CU, of 16 waves that each fill a list (with 4 waves 24).  One row of
-// 65536: 12 us in two launches, chains of dependent steps.  Tried and dropped:
-// values through LDS instead of 16 copies of the insertion (T = 1: 16.2 us
-// against 14.4), the waves of a row sharing their bounds (16.1 against 13.5), the
-// next step's loads ahead (no gain).
+// by memory, the vector ALU 88 % busy.  16384 x 1000 int32, 5 alternatives:
+// 22.6-25 us, 14 without: a wave per row, 453 vector and 415 scalar instructions
+// of which the sums are 200.  301 x 50021 fp32, 8 alternatives: 20 us, 14
+// without: 1.2 rows per CU, of 16 waves that each fill a list.  One row of 65536:
+// 11.6 us in two launches, chains of dependent steps.  Tried and dropped: values
+// through LDS instead of 16 copies of the insertion (one row: 16.2 us against
+// 14.4), the waves of a row sharing their bounds (16.1 against 13.5), the next
+// step's loads ahead (no gain).
 #include "dtypes.hpp"
 #include "quant.hpp"
 #include "wave_ops.hpp"

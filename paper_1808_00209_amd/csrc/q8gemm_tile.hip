@@ -19,9 +19,11 @@
 // busy in 60 % of the cycles.  Tried there: four waves of 128 x 128 (half the
 // LDS reads; 488 us against 490), bands of 2 to 16 row tiles (497-506).  Outputs
 // stored by each lane as they came took 640 us: through LDS they leave in runs.
-// 256 x 4096 outputs, K 4096 (a tile of 64 per CU): 9.9 us, of which the 32
-// stages' loads and barriers are about 6 (their wait counted, so that two later
-// stages stay on their way: 17.8 us without; K split over the waves: 10.6).
+// 256 x 4096 outputs, K 4096 (a tile of 64 per CU): 10 us, 3.3 of start and end
+// and 0.18-0.2 per stage of 16 KB, 38 bytes a cycle into the CU's LDS (the wait
+// for a stage's loads is counted, so that two later stages stay on their way:
+// 17.8 us without).  Tried there: K split over the waves (10.6), stages of 256
+// bytes (11.1), six stages (10.9).
 #include "q8gemm.hpp"
 
 namespace bnn {
@@ -58,7 +60,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4 * (TM * TN < 8 ? 2 : 1)) 
   const int64_t m0 = static_cast<int64_t>(b * band + in % high) * BM;
   const int n0 = in / high * BN;
 
-  // Thread i of a stage's load l fills LDS slot l * 256 + i: chunk
+  // Thread i of a stage's load l fills LDS slot l * kNT + i: chunk
   // (slot % 8) ^ (row / 2 % 8) of row slot / 8.
   const int8_t* src[kLoads];
 #pragma unroll
