@@ -570,16 +570,21 @@ __global__ __launch_bounds__(64) void join_kernel(LogprobsArgs a, int splits) {
   write_row<T>(a, t, s, static_cast<uint64_t>(top.hi) << 32 | top.lo, factor_of(a.scale), given);
 }
 
-// From kFull rows on, each is one workgroup's (or wave's): 1024 x 32768 25 us, in
-// parts and joined 33.  Fewer are split into parts of 4 steps or more per wave
-// (one row of 65536: 12.2 us; as one workgroup of 16 waves 22, in parts of a
-// quarter each 14).  Long rows that leave CUs with one or two workgroups go to 16
-// waves (301 x 50021: 22 us, 4 waves 24).
-constexpr int kFull = 256;
+// From kFull rows on, each is one workgroup's (or wave's): 200 x 50021 fp32 15.4
+// us, in parts and joined 19.3; 255 x 65536 bf16 17.3 : 21.3, but 128 x 131072
+// 23.8 : 20.9.  Fewer are split into parts of 4 steps or more per wave, if there
+// are three (one row of 65536: 12 us; as one workgroup of 16 waves 22; 64 x 8000
+// in two parts 10.3, whole 9.0).  Long rows that leave CUs with one or two
+// workgroups go to 16 waves (301 x 50021: 20 us, 4 waves 24).
+constexpr int kFull = 160;
+constexpr int kLongFew = 512;       // rows, below which long ones have 16 waves
 constexpr int kParts = 1024;        // parts that fill the card
 constexpr int kLength = 4 * kStep;  // a part's values, at least
 
-int64_t most_splits(int32_t V) { return (V + kLength - 1) / kLength; }
+int64_t most_splits(int32_t V) {
+  const int64_t n = (V + kLength - 1) / kLength;
+  return n < 3 ? 1 : n;
+}
 int64_t splits_of(int64_t T, int32_t V) {
   if (T >= kFull) return 1;
   const int64_t want = (kParts + T - 1) / T;
@@ -610,7 +615,7 @@ hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t s) {
     };
     auto waves = [&](auto tc) {
       if (a.V <= 4096) with(std::integral_constant<int, 1>{}, tc);
-      else if (splits == 1 && a.T < 2 * kFull && a.V >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
+      else if (splits == 1 && a.T < kLongFew && a.V >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
       else with(std::integral_constant<int, 4>{}, tc);
     };
     if (a.top_k > 0) waves(std::true_type{});
