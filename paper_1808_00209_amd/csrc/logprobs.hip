@@ -614,7 +614,9 @@ hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t s) {
           <<<static_cast<unsigned>((parts + per - 1) / per), W > 4 ? W * 64 : kNT, 0, s>>>(a, splits, length);
     };
     auto waves = [&](auto tc) {
-      if (a.V <= 4096) with(std::integral_constant<int, 1>{}, tc);
+      // (a wave per row, of one step or where there are rows for all waves:
+      // 4000 x 4096 bf16 16.2 us, four waves 18.9; 1000 x 4096 11.1 : 8.6)
+      if (a.V <= kStep || (a.V <= 4 * kStep && a.T >= 2048)) with(std::integral_constant<int, 1>{}, tc);
       else if (splits == 1 && a.T < kLongFew && a.V >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
       else with(std::integral_constant<int, 4>{}, tc);
     };

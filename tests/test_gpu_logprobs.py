@@ -61,7 +61,7 @@ def _logits(g, T, V, kind, spread=4.0):
 
 
 SIZES = [(1, 1), (2, 2), (1, 7), (5, 8), (3, 63), (300, 65), (4, 511), (7, 512), (2, 513), (1500, 1000), (5, 2047),
-         (3, 4096), (9, 4097), (1, 10000), (2, 32768), (1, 65536), (40, 5003), (3, 131072), (1100, 4500)]
+         (3, 4096), (9, 4097), (1, 10000), (2, 32768), (1, 65536), (40, 5003), (3, 131072), (1100, 4500), (2050, 1030), (2100, 4000)]
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
