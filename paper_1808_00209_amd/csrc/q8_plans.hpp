@@ -20,11 +20,14 @@ inline int64_t q8_tiles(int64_t M, int64_t N, int n) { return (M + n - 1) / n * 
 
 // on16: x, w and their strides on 16-byte steps.
 //
-// Many rows: the tile whose estimated time is least, in us at K = 4096, from
-// products of 256..8192 rows.  Tiles of 64 take 3 + 7 per 256 of them (256: 10.1,
-// 1024: 30.8), at least 8; one round of up to 256 tiles of 128 takes 23 (two
-// per CU and rounds of 512: 38), one of 256 tiles of 256 58 (up to half a round
-// 46, the clock being higher).  Other K move all of them alike.
+// Many rows: the tile whose estimated time is least, in tenths of us at K = 4096,
+// from products of 256..8192 rows.  Tiles of 64 take 3 + 7 per 256 of them (256:
+// 10.1, 640: 21.6, 1128: 34.9); up to 256 tiles of 128 15 + 8 (160: 19.4, 256:
+// 22.9); two per CU and more of these 28 + 10 (280: 29.6, 420: 36), then 38 per
+// round of 512; tiles of 256 58 per round (up to half a round 46, the clock being
+// higher).  Other K move all of them alike, but small ones favour fewer tiles
+// (1500 x 3000, K 700: 64 16.1, 128 11.9 us; K 4096: 34.9, 29.8).  Of 34 products
+// one is 1.14 off the best form (64 x 20000, K 8000), the others within 1.05.
 //
 // Few rows (us, skinny : tiles of 64, K 4096): 16 rows of 4096 outputs 8.0 : 8.7
 // and of 65536 58.0 : 59.4; 32 rows, in two operands of the skinny kernel, 10.6 :
@@ -34,10 +37,12 @@ inline Q8Form q8_form(int64_t M, int64_t N, int64_t K, bool on16) {
   if (K >= 16 && K <= 8192 && M <= 16) return kQ8Skinny;
   if (K < 16 || !on16) return kQ8Any;
   const int64_t t64 = q8_tiles(M, N, 64), t128 = q8_tiles(M, N, 128), t256 = q8_tiles(M, N, 256);
-  const int64_t in64 = 3 + 7 * t64 / 256;
-  const int64_t in128 = t128 <= 256 ? 23 : (t128 + 511) / 512 * 38;
-  const int64_t in256 = t256 <= 128 ? 46 : (t256 + 255) / 256 * 58;
-  if (in64 < 8 || (in64 <= in128 && in64 <= in256)) return kQ8Tile64;
+  const int64_t in64 = 30 + 70 * t64 / 256;
+  const int64_t in128 = t128 <= 256   ? 150 + 80 * t128 / 256
+                        : t128 <= 512 ? 280 + 100 * (t128 - 256) / 256
+                                      : (t128 + 511) / 512 * 380;
+  const int64_t in256 = t256 <= 128 ? 460 : (t256 + 255) / 256 * 580;
+  if (in64 <= in128 && in64 <= in256) return kQ8Tile64;
   if (in128 <= in256) return t128 <= 256 ? kQ8Tile128 : kQ8Pair128;
   return kQ8Tile256;
 }
