@@ -616,14 +616,16 @@ def _output(t, like, shape, dtype, name, stream):
 def _rows(t, name):
     """A 2-d tensor whose rows are contiguous and do not overlap: their distance
     in elements."""
-    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+    strides = t.stride()
+    if len(strides) != 2 or not t.is_cuda or (strides[1] != 1 and t.shape[1] > 1):
         raise ValueError("%s must be a 2-d CUDA(HIP) tensor with contiguous rows" % name)
-    if t.shape[0] < 2:
-        return t.shape[1]
-    if t.stride(0) < t.shape[1]:
+    n, d = t.shape
+    if n < 2:
+        return d
+    if strides[0] < d:
         raise ValueError("the rows of %s overlap (%d elements long, %d apart): call contiguous()"
-                         % (name, t.shape[1], t.stride(0)))
-    return t.stride(0)
+                         % (name, d, strides[0]))
+    return strides[0]
 
 
 # (The sizes of workspaces are functions of the call's sizes alone: asked for
@@ -804,13 +806,13 @@ def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=N
 # ----------------------------------------- 8-bit layers and their answers ---
 def _together(like, *others):
     """Every tensor of a call lies on the current device, like the stream."""
-    at = like.device
+    at = like.get_device()
     for t in others:
-        if t is not None and t.device != at:
-            raise ValueError("tensors on %s and on %s in one call" % (at, t.device))
-    if _raw_device is not None and at.index is not None and at.index != _raw_device():
+        if t is not None and t.get_device() != at:
+            raise ValueError("tensors on %s and on %s in one call" % (like.device, t.device))
+    if at >= 0 and _raw_device is not None and at != _raw_device():
         raise ValueError("tensors on %s, but the current device is cuda:%d: use torch.cuda.device"
-                         % (at, _raw_device()))
+                         % (like.device, _raw_device()))
 
 
 def _rows8(like, M, D, stream):

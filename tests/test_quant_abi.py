@@ -2,6 +2,7 @@
 argument gives its status and text before anything is launched (CPU only: the
 pointers are never read), and the binding's own checks."""
 import ctypes
+import types
 
 import pytest
 import torch
@@ -164,8 +165,11 @@ def test_binding_checks():
             call()
 
 
-def test_tensors_of_one_device():
-    a, b = _made(4, 8), torch.zeros(4, device="meta")
+def test_tensors_of_one_device(monkeypatch):
+    on = lambda i: types.SimpleNamespace(get_device=lambda: i, device="cuda:%d" % i)  # noqa: E731
+    monkeypatch.setattr(bnn, "_raw_device", lambda: 1)
+    bnn._together(on(1), None, on(1))
     with pytest.raises(ValueError, match="in one call"):
-        bnn._together(a, None, b)
-    bnn._together(a, None, _made(3))
+        bnn._together(on(1), None, on(0))
+    with pytest.raises(ValueError, match="current device"):
+        bnn._together(on(0), on(0))
