@@ -5,7 +5,7 @@
 //   s1 = sum 2^d,  s2 = sum 2^d d,   d = c v - ref,
 //   ln p_v = (c v - ref - log2 s1) ln 2,   entropy = (log2 s1 - s2 / s1) ln 2.
 // ref is any number near the largest c v: it is taken from the first values and
-// moved (s1 and s2 with it) only when a value lies 2^60 above it, so that a
+// moved (s1 and s2 with it) only when a value lies 2^16 above it, so that a
 // value costs one fma, one exp2 and two sums, and no maximum of its own.
 //
 // The alternatives so far are a sorted list over the wave's lanes, one 64-bit
@@ -37,7 +37,9 @@ namespace {
 constexpr int kNT = 256;  // unless a row has more waves
 constexpr int kEach = 16;          // values of a lane per step, in groups of 8
 constexpr int kStep = 64 * kEach;  // of a wave
-constexpr float kAway = 60.0f;     // a value this far above the reference moves it
+// A value this far above the reference moves it: log2 s1 and s2 / s1 stay below
+// 16 + log2 V, so that their difference loses few bits.
+constexpr float kAway = 16.0f;
 constexpr float kFar = 3e38f;    // the reference before there is one: minus this
 constexpr float kLarge = 0x1p20f; // the quick form's references, at most
 
@@ -464,7 +466,7 @@ __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t t, cons
   constexpr double kLn2 = 0.693147180559945309417;
   const int lane = threadIdx.x & 63;
   const bool none = s.s1 == 0.0f, bad = !(s.s1 < __builtin_inff());
-  // (2^-60 <= s1 < 2^24 2^60, or 1 <= s1 <= 2^24 by the safe form)
+  // (the largest value's part is 1 or more, but for the reference's rounding)
   const float ls = __builtin_amdgcn_logf(s.s1);
   const float ref = static_cast<float>(s.ref);
   const bool quick = static_cast<double>(ref) == s.ref && __builtin_fabsf(ref) <= kLarge;

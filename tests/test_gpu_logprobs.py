@@ -239,3 +239,14 @@ def test_many_given(n):
     for T, V in ((2, 900), (1, 40000), (300, 6000)):
         ids = torch.randint(-2, V + 2, (T, n), generator=g, dtype=torch.int32)
         _check(_logits(g, T, V, "fp32"), ids, 2)
+
+
+@pytest.mark.parametrize("V", [3000, 20000, 140000])
+@pytest.mark.parametrize("rise", [0.5, 9.0, 15.0, 300.0])
+def test_rising_rows(V, rise):
+    """Rows whose largest values come last, far above the first ones: the
+    reference moves, or stays just below them."""
+    g = torch.Generator().manual_seed(V + 4)
+    up = torch.arange(V) * (rise / V)
+    z = torch.stack([up, (torch.arange(V) >= V - 5) * rise, up + 0.01 * torch.randn(V, generator=g)]).float()
+    _check(z, torch.randint(0, V, (3, 2), generator=g, dtype=torch.int32), 7)
