@@ -487,12 +487,14 @@ __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t t, cons
     if (std::is_same<R, float>::value && static_cast<float>(v) == -__builtin_inff())
       return -__builtin_inff();
     const float d = __builtin_fmaf(static_cast<float>(v), c, -ref);
-    if (quick && __builtin_fabsf(d) < 1e30f) return (d - ls) * static_cast<float>(kLn2);
-    return static_cast<float>((static_cast<double>(v) * c - s.ref - static_cast<double>(ls)) * kLn2);
+    const float lp = quick && __builtin_fabsf(d) < 1e30f
+        ? (d - ls) * static_cast<float>(kLn2)
+        : static_cast<float>((static_cast<double>(v) * c - s.ref - static_cast<double>(ls)) * kLn2);
+    return __builtin_fminf(lp, 0.0f);  // (roundings may pass 0)
   };
   if (a.entropy && lane == 0)
     a.entropy[t] = bad ? nan : none ? 0.0f
-        : (ls - s.s2 / s.s1) * static_cast<float>(kLn2);
+        : __builtin_fmaxf((ls - s.s2 / s.s1) * static_cast<float>(kLn2), 0.0f);
   for (int j = lane; j < a.n; j += 64) {
     if (j >= 64) {
       given.id = a.ids[t * a.n + j];

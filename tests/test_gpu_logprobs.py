@@ -37,6 +37,9 @@ def _check(logits, ids=None, top_k=0, logit_scale=1.0, dev=None):
     got = bnn.bnn_logprobs(dev, None if ids is None else ids.cuda(), top_k, logit_scale)
     torch.cuda.synchronize()
     given, entropy, top_ids, top = ref.logprobs(logits, ids, top_k, logit_scale)
+    for t in got[:2] + got[3:]:
+        assert t is None or not (t > 0).any() or t is got[1]
+    assert not (got[1] < 0).any()
     V = logits.shape[1]
     Z = 0.0
     for v in (given, top):
@@ -250,3 +253,11 @@ def test_rising_rows(V, rise):
     up = torch.arange(V) * (rise / V)
     z = torch.stack([up, (torch.arange(V) >= V - 5) * rise, up + 0.01 * torch.randn(V, generator=g)]).float()
     _check(z, torch.randint(0, V, (3, 2), generator=g, dtype=torch.int32), 7)
+
+
+def test_certain_rows():
+    """One answer far above the others: ln p at most 0, entropy at least 0."""
+    z = 0.01 * torch.randn(64, 1000, generator=torch.Generator().manual_seed(17))
+    z[torch.arange(64), torch.arange(64) * 15] += torch.linspace(5, 60, 64)
+    _check(z, (torch.arange(64) * 15).to(torch.int32), 3)
+    _check(z.repeat(1, 30), (torch.arange(64) * 15).to(torch.int32), 3, 3.0)
