@@ -13,6 +13,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import operator
 import os
 
 import torch
@@ -679,7 +680,7 @@ def bnn_group_rows(ids, G, offsets=None, order=None, workspace=None, stream=None
     last."""
     lib = load()
     _dev(ids, torch.int32, "ids")
-    M = ids.numel()
+    M, G = ids.numel(), operator.index(G)  # (a key of the workspace's size)
     offsets = _output(offsets, ids, (G + 1,), torch.int32, "offsets", stream)
     order = _output(order, ids, (M,), torch.int32, "order", stream)
     workspace, n = _workspace(workspace, _group_rows_bytes(M, G), ids, stream)
@@ -822,7 +823,9 @@ def _rows8(like, M, D, stream):
     return _empty(like, (M, (D + 15) // 16 * 16), torch.int8, stream)[:, :D]
 
 
-# (A call's description is a function of its sizes: made once for each.)
+# (A call's description is a function of its sizes: made once for each.  Keys
+# are plain numbers: a tensor would be found again by its identity, whatever it
+# holds by then.)
 @functools.lru_cache(maxsize=1024)
 def _desc(kind, *fields):
     return ctypes.byref(kind(*fields))
@@ -872,7 +875,7 @@ def bnn_rmsnorm(x, weight=None, residual=None, eps=1e-6, want_y=False, want_q=Tr
         scale = _output(scale, x, (M,), torch.float32, "scale", stream)
     elif scale is not None:
         raise ValueError("scale goes with q")
-    d = _desc(RmsnormDesc, M, D, code, w_code, eps)
+    d = _desc(RmsnormDesc, M, D, code, w_code, float(eps))
     _check(lib.bnn_rmsnorm(d, _ptr(x), stride, _ptr(residual), r_stride,
                            _ptr(weight), _ptr(sum), _ptr(y), _ptr(q), q_stride, _ptr(scale),
                            _stream(stream)))
@@ -929,6 +932,7 @@ def bnn_logprobs(logits, ids=None, top_k=0, logit_scale=1.0, want_entropy=True, 
         raise TypeError("logits must be float32, float16, bfloat16 or int32")
     stride = _rows(logits, "logits")
     T, V = logits.shape
+    top_k, logit_scale = operator.index(top_k), float(logit_scale)
     _together(logits, ids, logp, entropy, top_ids, top_logp, workspace)
     n = 0
     if ids is not None:
