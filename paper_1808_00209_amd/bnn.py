@@ -85,33 +85,54 @@ class Layer(ctypes.Structure):
                 ("flip", ctypes.c_void_p), ("offset", ctypes.c_void_p), ("wprep", ctypes.c_void_p)]
 
 
-class RouteDesc(ctypes.Structure):
+def _fitting(value, name):
+    """A 32-bit size (ctypes takes the low 32 bits of any other)."""
+    if not -1 << 31 <= value < 1 << 31:
+        raise ValueError("%s is %d: beyond 32 bits" % (name, value))
+    return value
+
+
+class _Desc(ctypes.Structure):
+    """A call's description.  ctypes takes a large number's low bits without a
+    word, so that a size that its field does not hold is refused here."""
+
+    def __init__(self, *fields, **named):
+        super().__init__(*fields, **named)
+        if not named and max(fields, default=0) < 1 << 31 and min(fields, default=0) >= -1 << 31:
+            return
+        for (name, kind), value in [*zip(self._fields_, fields),
+                                    *((f, named[f[0]]) for f in self._fields_ if f[0] in named)]:
+            if kind is not ctypes.c_float and getattr(self, name) != value:
+                raise ValueError("%s is %d: beyond %d bits" % (name, value, 8 * ctypes.sizeof(kind)))
+
+
+class RouteDesc(_Desc):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("E", "top_k", "groups", "top_groups", "group_top", "score", "renorm", "dtype")]
     _fields_ += [("scale", ctypes.c_float), ("logit_scale", ctypes.c_float)]
 
 
-class ExpertsDesc(ctypes.Structure):
+class ExpertsDesc(_Desc):
     _fields_ = [("T", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in
                                           ("top_k", "E", "N", "K", "share")]
 
 
-class LoraDesc(ctypes.Structure):
+class LoraDesc(_Desc):
     _fields_ = [("M", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in
                                           ("N", "K", "adapters", "rank", "dtype", "out_dtype")]
 
 
-class RmsnormDesc(ctypes.Structure):
+class RmsnormDesc(_Desc):
     _fields_ = [("M", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in
                                           ("D", "dtype", "weight_dtype")]
     _fields_ += [("eps", ctypes.c_float)]
 
 
-class Q8gemmDesc(ctypes.Structure):
+class Q8gemmDesc(_Desc):
     _fields_ = [("M", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("N", "K", "dtype")]
 
 
-class LogprobsDesc(ctypes.Structure):
+class LogprobsDesc(_Desc):
     _fields_ = [("T", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in
                                           ("V", "n", "top_k", "dtype")]
     _fields_ += [("logit_scale", ctypes.c_float)]
@@ -639,6 +660,14 @@ def _workspace(ws, need, like, stream):
     return ws, _dev(ws, torch.uint8, "workspace").numel()
 
 
+# (A call's description is a function of its sizes: made and looked at once for
+# each.  Keys are plain numbers: a tensor would be found again by its identity,
+# whatever it holds by then.)
+@functools.lru_cache(maxsize=1024)
+def _kept_desc(kind, *fields):
+    return kind(*fields)
+
+
 def bnn_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=None, group_top=1,
               renormalize=True, scale=1.0, logit_scale=1.0, ids=None, weights=None, stream=None):
     """Routing: logits [T, E] (float32, float16, bfloat16 or int32; rows may be
@@ -658,8 +687,10 @@ def bnn_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=No
     weights = _output(weights, logits, (T, top_k), torch.float32, "weights", stream)
     if score not in _SCORES:
         raise ValueError("score must be one of %s" % sorted(_SCORES))
-    d = RouteDesc(E, top_k, groups, groups if top_groups is None else top_groups, group_top,
-                  _SCORES[score], bool(renormalize), dtype, scale, logit_scale)
+    counts = [operator.index(n) for n in
+              (top_k, groups, groups if top_groups is None else top_groups, group_top)]
+    d = _kept_desc(RouteDesc, E, *counts, _SCORES[score], bool(renormalize), dtype, float(scale),
+                   float(logit_scale))
     _check(lib.bnn_route(ctypes.byref(d), T, _ptr(logits), stride, _ptr(bias), _ptr(ids),
                          _ptr(weights), _stream(stream)))
     return ids, weights
@@ -667,7 +698,7 @@ def bnn_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=No
 
 def bnn_group_rows_workspace_size(M, G) -> int:
     out = ctypes.c_size_t()
-    _check(load().bnn_group_rows_workspace_size(M, G, ctypes.byref(out)))
+    _check(load().bnn_group_rows_workspace_size(M, _fitting(G, "G"), ctypes.byref(out)))
     return out.value
 
 
@@ -680,7 +711,7 @@ def bnn_group_rows(ids, G, offsets=None, order=None, workspace=None, stream=None
     last."""
     lib = load()
     _dev(ids, torch.int32, "ids")
-    M, G = ids.numel(), operator.index(G)  # (a key of the workspace's size)
+    M, G = ids.numel(), _fitting(operator.index(G), "G")
     offsets = _output(offsets, ids, (G + 1,), torch.int32, "offsets", stream)
     order = _output(order, ids, (M,), torch.int32, "order", stream)
     workspace, n = _workspace(workspace, _group_rows_bytes(M, G), ids, stream)
@@ -699,7 +730,7 @@ def _experts_desc(x, K, w, M, top_k, offsets, order):
         raise ValueError("x must be [%d or %d, %d] packed words of %d bits" % (T, M, words(K), K))
     _shaped(_dev(offsets, torch.int32, "offsets"), (E + 1,), "offsets")
     _shaped(_dev(order, torch.int32, "order"), (M,), "order")
-    return ExpertsDesc(T, top_k, E, N, K, int(top_k > 1 and x.shape[0] == T))
+    return _kept_desc(ExpertsDesc, T, top_k, E, N, operator.index(K), int(top_k > 1 and x.shape[0] == T))
 
 
 def bnn_experts_fc(x, K, w, offsets, order, thr, flip=None, out_bits=None, stream=None):
@@ -795,7 +826,7 @@ def bnn_bgemm_lora(x, w, ids, a, b, scale=None, alpha=None, offset=None, order=N
     dtype = out.dtype if out is not None else kind if dtype is None else dtype
     out_code = _real(dtype, "out")
     out = _output(out, x, (M, N), dtype, "out", stream)
-    d = LoraDesc(M, N, K, L, rank, code, out_code)
+    d = _kept_desc(LoraDesc, M, N, K, L, rank, code, out_code)
     workspace, n = _workspace(workspace, _lora_bytes(M, N, K, L, rank, code, out_code), x,
                               stream)
     _check(lib.bnn_bgemm_lora(ctypes.byref(d), _ptr(x), stride, _ptr(offset), _ptr(w),
@@ -821,14 +852,6 @@ def _rows8(like, M, D, stream):
     if D % 16 == 0:
         return _empty(like, (M, D), torch.int8, stream)
     return _empty(like, (M, (D + 15) // 16 * 16), torch.int8, stream)[:, :D]
-
-
-# (A call's description is a function of its sizes: made once for each.  Keys
-# are plain numbers: a tensor would be found again by its identity, whatever it
-# holds by then.)
-@functools.lru_cache(maxsize=1024)
-def _desc(kind, *fields):
-    return ctypes.byref(kind(*fields))
 
 
 def _int8_rows(t, name):
@@ -875,8 +898,8 @@ def bnn_rmsnorm(x, weight=None, residual=None, eps=1e-6, want_y=False, want_q=Tr
         scale = _output(scale, x, (M,), torch.float32, "scale", stream)
     elif scale is not None:
         raise ValueError("scale goes with q")
-    d = _desc(RmsnormDesc, M, D, code, w_code, float(eps))
-    _check(lib.bnn_rmsnorm(d, _ptr(x), stride, _ptr(residual), r_stride,
+    d = _kept_desc(RmsnormDesc, M, D, code, w_code, float(eps))
+    _check(lib.bnn_rmsnorm(ctypes.byref(d), _ptr(x), stride, _ptr(residual), r_stride,
                            _ptr(weight), _ptr(sum), _ptr(y), _ptr(q), q_stride, _ptr(scale),
                            _stream(stream)))
     return sum, y, q, scale
@@ -900,8 +923,8 @@ def bnn_q8gemm(x, w, x_scale=None, w_scale=None, bias=None, dtype=torch.float32,
     dtype = dtype if out is None else out.dtype
     code = _real(dtype, "out")
     out = _output(out, x, (M, N), dtype, "out", stream)
-    d = _desc(Q8gemmDesc, M, N, K, code)
-    _check(lib.bnn_q8gemm(d, _ptr(x), x_stride, _ptr(x_scale), _ptr(w), w_stride,
+    d = _kept_desc(Q8gemmDesc, M, N, K, code)
+    _check(lib.bnn_q8gemm(ctypes.byref(d), _ptr(x), x_stride, _ptr(x_scale), _ptr(w), w_stride,
                           _ptr(w_scale), _ptr(bias), _ptr(out), _stream(stream)))
     return out
 
@@ -949,9 +972,9 @@ def bnn_logprobs(logits, ids=None, top_k=0, logit_scale=1.0, want_entropy=True, 
         top_logp = _output(top_logp, logits, (T, top_k), torch.float32, "top_logp", stream)
     elif top_ids is not None or top_logp is not None:
         raise ValueError("top_ids and top_logp go with top_k")
-    d = _desc(LogprobsDesc, T, V, n, top_k, dtype, logit_scale)
+    d = _kept_desc(LogprobsDesc, T, V, n, top_k, dtype, logit_scale)
     workspace, size = _workspace(workspace, _logprobs_bytes(T, V, top_k), logits, stream)
-    _check(lib.bnn_logprobs(d, _ptr(logits), stride, _ptr(ids), _ptr(logp),
+    _check(lib.bnn_logprobs(ctypes.byref(d), _ptr(logits), stride, _ptr(ids), _ptr(logp),
                             _ptr(entropy), _ptr(top_ids), _ptr(top_logp), _ptr(workspace), size,
                             _stream(stream)))
     return logp, entropy, top_ids, top_logp
