@@ -773,8 +773,8 @@ typedef struct bnn_logprobs_desc {
  * value is a value as any other.  In a row with nothing in reach every logp is
  * -inf and the entropy 0.  A row that holds NaN or +inf: logp, entropy and
  * top_logp NaN, top_ids -1 (-inf stays for ids not in [0, V)).  Sums are held
- * in fp32; no ln p is above 0 and no entropy below.  int32 logits beyond 2^24
- * are rounded to fp32 in them, but not in their order.
+ * in fp32; no ln p is above 0 and no entropy below.  int32 logits count as the
+ * integers they are, beyond 2^24 too.
  *   logits  [T][V], rows `stride` elements apart (stride >= V), of d->dtype.
  *   ids     [T][n] int32 and logp [T][n] fp32, or both NULL with n == 0.
  *   entropy [T] fp32 or NULL.

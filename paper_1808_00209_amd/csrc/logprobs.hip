@@ -44,6 +44,11 @@ constexpr int kStep = 64 * kEach;  // of a wave
 constexpr float kAway = 16.0f;
 constexpr float kFar = 3e38f;    // the reference before there is one: minus this
 constexpr float kLarge = 0x1p20f; // the quick form's references, at most
+// The quick form takes integers as fp32.  Up to kExact the largest is itself, and
+// a smaller one's rounding 2^-24 of its distance; beyond it c v is off by up to
+// 2^-25 of itself, 2^-23 with references up to kSmall.
+constexpr float kExact = 0x1p23f;
+constexpr float kSmall = 4.0f;
 
 struct Sums {
   double ref;
@@ -179,43 +184,69 @@ __device__ __forceinline__ void raise_floor(Top& top, uint32_t mine, int top_k) 
 }
 
 // SAFE: the reference is the largest value itself and differences are taken
-// before the factor, for rows whose c v pass 2^20, rows without a value in reach
-// and rows with NaN or infinity (whose quick sums end as 0, NaN or infinity).
-template <bool SAFE>
+// before the factor, of integers as integers, for rows whose c v pass 2^20 (or
+// pass kSmall with integers beyond kExact), rows without a value in reach and
+// rows with NaN or infinity (whose quick sums end as 0, NaN or infinity).
+template <bool SAFE, class R>
 struct Scan {
-  float c, ref, s1, s2;
+  static constexpr bool kInts = std::is_same<R, int32_t>::value;
+  using Ref = std::conditional_t<SAFE, R, float>;
+  float c;
+  Ref ref;
+  float s1, s2;
 
   __device__ __forceinline__ void start(float factor) {
     c = factor;
-    ref = SAFE ? -__builtin_inff() : -kFar;
+    if constexpr (!SAFE) ref = -kFar;
+    else if constexpr (kInts) ref = INT32_MIN;
+    else ref = -__builtin_inff();
     s1 = s2 = 0.0f;
   }
-  __device__ __forceinline__ float delta(float v) const {
-    if constexpr (SAFE) return v == -__builtin_inff() ? v : (v - ref) * c;
-    else return __builtin_fmaf(v, c, -ref);
+  // c (from - to) of integers, from <= to.
+  __device__ __forceinline__ float fall(int32_t from, int32_t to) const {
+    return -static_cast<float>(static_cast<uint32_t>(to) - static_cast<uint32_t>(from)) * c;
   }
-  // The reference for values up to fm (of each lane).
-  __device__ __forceinline__ void refer(float fm) {
-    if (__any(SAFE ? fm > ref : delta(fm) > kAway)) {
-      const float top = wave_max(fm);
-      const float next = SAFE ? top : top * c;
-      // (a quick reference's own rounding must not count: 2^-5 at most)
-      if (!SAFE && !(__builtin_fabsf(next) <= kLarge)) s1 = __builtin_nanf("");
-      float move = SAFE ? (ref - next) * c : ref - next;
-      move = s1 == 0.0f ? -1e4f : __builtin_fmaxf(move, -1e4f);
-      const float f = exp2_of(move);
-      s2 = f * __builtin_fmaf(move, s1, s2);
-      s1 *= f;
-      ref = next;
+  // (SAFE: of a value that is not above the reference)
+  __device__ __forceinline__ float delta(R v) const {
+    if constexpr (!SAFE) return __builtin_fmaf(static_cast<float>(v), c, -ref);
+    else if constexpr (kInts) return fall(v, ref);
+    else return v == -__builtin_inff() ? v : (v - ref) * c;
+  }
+  // The reference for values up to m (of each lane that has some).
+  __device__ __forceinline__ void refer(R m, bool some) {
+    if constexpr (SAFE) {
+      if (__any(some && m > ref)) {
+        const R next = wave_max(some ? m : ref);
+        if constexpr (kInts) move_to(next, fall(ref, next));
+        else move_to(next, (ref - next) * c);
+      }
+    } else {
+      const float fm = some ? static_cast<float>(m) : -__builtin_inff();
+      if (__any(__builtin_fmaf(fm, c, -ref) > kAway)) {
+        const float top = wave_max(fm), next = top * c;
+        // (a quick reference's own rounding must not count: 2^-5 at most; nor an
+        // integer's: of 2^-24 c v, where one beyond kExact is asked for)
+        if (!(__builtin_fabsf(next) <= kLarge) ||
+            (kInts && __builtin_fabsf(top) > kExact && __builtin_fabsf(next) > kSmall))
+          s1 = __builtin_nanf("");
+        move_to(next, ref - next);
+      }
     }
   }
-  // FINITE: no value is -inf.
+  __device__ __forceinline__ void move_to(Ref next, float move) {
+    move = s1 == 0.0f ? -1e4f : __builtin_fmaxf(move, -1e4f);
+    const float f = exp2_of(move);
+    s2 = f * __builtin_fmaf(move, s1, s2);
+    s1 *= f;
+    ref = next;
+  }
+  // The first n of v (8 and more: all).  FINITE: no value is -inf.
   template <bool FINITE>
-  __device__ __forceinline__ void add(const float (&v)[8]) {
+  __device__ __forceinline__ void add(const R (&v)[8], int n) {
     float e[8], d[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      d[i] = delta(v[i]);
+      d[i] = i < n ? delta(v[i]) : -__builtin_inff();
       e[i] = exp2_of(d[i]);
       if (!FINITE) d[i] = __builtin_fmaxf(d[i], -200.0f);  // (0 * -inf)
     }
@@ -251,7 +282,7 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
   constexpr bool kInts = std::is_same<R, int32_t>::value;
   constexpr int kGroups = kEach / 8;
   const int lane = threadIdx.x & 63;
-  Scan<SAFE> sc;
+  Scan<SAFE, R> sc;
   sc.start(c);
   // A step: group g of a lane's 8 values starts at index at + 512 g + 8 lane.
   // What lies past the row's end is -inf; integers have no such value, so there
@@ -270,17 +301,14 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
       for (int i = 1; i < kEach; ++i) m = __builtin_fmaxf(m, v[i]);
     }
     const bool some = kPart == kAll || n[0] > 0;  // (past the end: the least integer)
-    sc.refer(some ? static_cast<float>(m) : -__builtin_inff());
+    sc.refer(m, some);
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
       if (kPart == kWhole && n[g] <= 0) continue;
-      float f[8];
+      R f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        f[i] = static_cast<float>(v[8 * g + i]);
-        if (kPart == kSome) f[i] = i < n[g] ? f[i] : -__builtin_inff();
-      }
-      sc.template add<kInts && kPart != kSome>(f);
+      for (int i = 0; i < 8; ++i) f[i] = v[8 * g + i];
+      sc.template add<kInts && kPart != kSome>(f, kPart == kSome ? n[g] : 8);
     }
     if constexpr (TOP) {
       // (a full list of earlier values: one that is equal to its last is behind)
@@ -487,7 +515,8 @@ __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t t, cons
     if (std::is_same<R, float>::value && static_cast<float>(v) == -__builtin_inff())
       return -__builtin_inff();
     const float d = __builtin_fmaf(static_cast<float>(v), c, -ref);
-    const float lp = quick && __builtin_fabsf(d) < 1e30f
+    const bool as_is = std::is_same<R, float>::value || (v >= -(1 << 24) && v <= 1 << 24);
+    const float lp = quick && as_is && __builtin_fabsf(d) < 1e30f
         ? (d - ls) * static_cast<float>(kLn2)
         : static_cast<float>((static_cast<double>(v) * c - s.ref - static_cast<double>(ls)) * kLn2);
     return __builtin_fminf(lp, 0.0f);  // (roundings may pass 0)

@@ -61,6 +61,9 @@ __device__ __forceinline__ T wave_sum(T v) {
 __device__ __forceinline__ float wave_max(float v) {
   return wave_reduce(v, [](float a, float b) { return __builtin_fmaxf(a, b); });
 }
+__device__ __forceinline__ int32_t wave_max(int32_t v) {
+  return wave_reduce(v, [](int32_t a, int32_t b) { return a > b ? a : b; });
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return wave_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
