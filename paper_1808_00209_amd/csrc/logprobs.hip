@@ -49,6 +49,9 @@ constexpr float kLarge = 0x1p20f; // the quick form's references, at most
 // 2^-25 of itself, 2^-23 with references up to kSmall.
 constexpr float kExact = 0x1p23f;
 constexpr float kSmall = 4.0f;
+// Integers that differ at all have no sums in common from 2^8 on: factors are cut
+// to this one in them, so that no product passes fp32's range (0 * inf).
+constexpr float kSharp = 0x1p90f;
 
 struct Sums {
   double ref;
@@ -191,12 +194,12 @@ template <bool SAFE, class R>
 struct Scan {
   static constexpr bool kInts = std::is_same<R, int32_t>::value;
   using Ref = std::conditional_t<SAFE, R, float>;
-  float c;
+  float c;  // (of integers at most kSharp)
   Ref ref;
   float s1, s2;
 
   __device__ __forceinline__ void start(float factor) {
-    c = factor;
+    c = kInts ? __builtin_fminf(factor, kSharp) : factor;
     if constexpr (!SAFE) ref = -kFar;
     else if constexpr (kInts) ref = INT32_MIN;
     else ref = -__builtin_inff();
@@ -226,9 +229,8 @@ struct Scan {
         const float top = wave_max(fm), next = top * c;
         // (a quick reference's own rounding must not count: 2^-5 at most; nor an
         // integer's: of 2^-24 c v, where one beyond kExact is asked for)
-        if (!(__builtin_fabsf(next) <= kLarge) ||
-            (kInts && __builtin_fabsf(top) > kExact && __builtin_fabsf(next) > kSmall))
-          s1 = __builtin_nanf("");
+        const float most = kInts && __builtin_fabsf(top) > kExact ? kSmall : kLarge;
+        if (!(__builtin_fabsf(next) <= most)) s1 = __builtin_nanf("");
         move_to(next, ref - next);
       }
     }
@@ -256,8 +258,9 @@ struct Scan {
     for (int i = 1; i < 8; ++i) t = __builtin_fmaf(e[i], d[i], t);
     s2 += t;
   }
-  __device__ __forceinline__ Sums total() const {
-    return {SAFE ? static_cast<double>(ref) * c : static_cast<double>(ref), wave_sum(s1),
+  // (a quick reference with a factor beyond kSharp is 0)
+  __device__ __forceinline__ Sums total(float factor) const {
+    return {SAFE ? static_cast<double>(ref) * factor : static_cast<double>(ref), wave_sum(s1),
             wave_sum(s2)};
   }
 };
@@ -400,7 +403,7 @@ __device__ __forceinline__ Sums scan(const T* row, int begin, int end, int wave,
     if (kInts && (end - at) % 8 == 0) step(v, at, n, std::integral_constant<int, kWhole>{});
     else step(v, at, n, std::integral_constant<int, kSome>{});
   }
-  return sc.total();
+  return sc.total(c);
 }
 
 // A wave's sums: in fp32's range by the quick form, or else by the safe one.
@@ -514,16 +517,17 @@ __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t t, cons
   auto ln_p = [&](R v) {
     if (std::is_same<R, float>::value && static_cast<float>(v) == -__builtin_inff())
       return -__builtin_inff();
-    const float d = __builtin_fmaf(static_cast<float>(v), c, -ref);
-    const bool as_is = std::is_same<R, float>::value || (v >= -(1 << 24) && v <= 1 << 24);
+    const float f = static_cast<float>(v), d = __builtin_fmaf(f, c, -ref);
+    const bool as_is = std::is_same<R, float>::value || __builtin_fabsf(f) < 0x1p24f;
     const float lp = quick && as_is && __builtin_fabsf(d) < 1e30f
         ? (d - ls) * static_cast<float>(kLn2)
         : static_cast<float>((static_cast<double>(v) * c - s.ref - static_cast<double>(ls)) * kLn2);
-    return __builtin_fminf(lp, 0.0f);  // (roundings may pass 0)
+    return lp > 0.0f ? 0.0f : lp;  // (roundings may pass 0)
   };
+  auto not_below_0 = [](float h) { return h < 0.0f ? 0.0f : h; };
   if (a.entropy && lane == 0)
     a.entropy[t] = bad ? nan : none ? 0.0f
-        : __builtin_fmaxf((ls - s.s2 / s.s1) * static_cast<float>(kLn2), 0.0f);
+        : not_below_0((ls - s.s2 / s.s1) * static_cast<float>(kLn2));
   for (int j = lane; j < a.n; j += 64) {
     if (j >= 64) {
       given.id = a.ids[t * a.n + j];

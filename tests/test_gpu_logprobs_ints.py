@@ -73,3 +73,37 @@ def test_dense_rows(T, V, scale):
     z = base[torch.arange(T) % 5][:, None] + torch.randint(0, wide + 1, (T, V), generator=g)
     z = z.clamp(-2 ** 31, 2 ** 31 - 1).to(torch.int32)
     _check(z, torch.randint(0, V, (T, 3), generator=g, dtype=torch.int32), 9, scale)
+
+
+@pytest.mark.parametrize("T, V", [(9, 8), (9, 24), (9, 1000), (9, 1001), (9, 5000), (9, 70000), (180, 16400)])
+@pytest.mark.parametrize("power", [9, 40, 89, 90, 91, 96, 97, 100])
+def test_far_factors(T, V, power):
+    """Factors that leave nothing but the largest: its ties share the row.  ln p
+    of the others is -scale * difference, off by the factor's rounding and twice
+    that of 31 bits times 24 in 64 bits (2^-52 |c v| each): 2^-23 of it and 2^-51
+    scale |v|."""
+    g = torch.Generator().manual_seed(V + power)
+    scale = 2.0 ** power
+    z = torch.randint(-2 ** 30, -2 ** 29, (T, V), generator=g).to(torch.int32)
+    tops = [0, 0, 2 ** 30, 2 ** 31 - 1, -2 ** 29, 7, 2 ** 25 + 1, -5, 2 ** 31 - 1]
+    lows = [-2 ** 31, -1, -2 ** 30, -2 ** 31, -2 ** 31, 6, 2 ** 25, -2 ** 31, 2 ** 31 - 2]
+    ids = torch.empty(T, 4, dtype=torch.int32)
+    for t in range(T):
+        if t % 9 in (0, 3):
+            z[t] = -2 ** 31
+        at = torch.randperm(V, generator=g)[:6]
+        z[t, at[:1 + t % 4]] = tops[t % 9]  # ties
+        z[t, at[4:]] = lows[t % 9]
+        ids[t] = torch.stack([at[0], at[4], at[5], torch.tensor(3)])
+    got = bnn.bnn_logprobs(z.cuda(), ids.cuda(), 5, scale)
+    given, entropy, top_ids, top = ref.logprobs(z, ids, 5, scale)
+    assert torch.equal(got[2].cpu(), top_ids)
+    ties = 1 + torch.arange(T) % 4
+    assert ((entropy - torch.log(ties.double())).abs() < 1e-9).all()
+    _near(got[1], entropy, 2.0 ** -20)  # (s1 and s2 exact, the log's 2 units of at most 2)
+    slack = 2.0 ** -20 + 2.0 ** -51 * scale * z.abs().max(1).values.clamp_min(1)[:, None].double()
+    for a, b in ((got[0], given), (got[3], top)):
+        a = a.cpu().double()
+        lost = b < -3.4e38
+        assert ((a - b).abs() <= slack + 2.0 ** -23 * b.abs())[~lost].all()
+        assert (a[lost] < -3.3e38).all()
