@@ -28,6 +28,7 @@
 // 14.4), the waves of a row sharing their bounds (16.1 against 13.5), the next
 // step's loads ahead (no gain).
 #include "dtypes.hpp"
+#include "logprobs_plans.hpp"
 #include "quant.hpp"
 #include "wave_ops.hpp"
 
@@ -39,6 +40,7 @@ namespace {
 constexpr int kNT = 256;  // unless a row has more waves
 constexpr int kEach = 16;          // values of a lane per step, in groups of 8
 constexpr int kStep = 64 * kEach;  // of a wave
+static_assert(kStep == kLogprobsStep, "the plans count in steps");
 // A value this far above the reference (2^2.5 times it) moves it, so that the
 // largest one's d, which log2 s1 and s2 / s1 share, has few bits before the
 // point: with 16 an almost certain answer's ln p was off by up to 7e-7 and the
@@ -623,40 +625,15 @@ __global__ __launch_bounds__(64) void join_kernel(LogprobsArgs a, int splits) {
   write_row<T>(a, t, s, static_cast<uint64_t>(top.hi) << 32 | top.lo, factor_of(a.scale), given);
 }
 
-// From kFull rows on, each is one workgroup's (or wave's): 200 x 50021 fp32 15.4
-// us, in parts and joined 19.3; 255 x 65536 bf16 17.3 : 21.3, but 128 x 131072
-// 23.8 : 20.9.  Fewer are split into parts of 4 steps or more per wave, if there
-// are three (one row of 65536: 12 us; as one workgroup of 16 waves 22; 64 x 8000
-// in two parts 10.3, whole 9.0).  Long rows that leave CUs with one or two
-// workgroups go to 16 waves (301 x 50021: 20 us, 4 waves 24).
-constexpr int kFull = 160;
-constexpr int kLongFew = 512;       // rows, below which long ones have 16 waves
-constexpr int kParts = 1024;        // parts that fill the card
-constexpr int kLength = 4 * kStep;  // a part's values, at least
-
-int64_t most_splits(int32_t V) {
-  const int64_t n = (V + kLength - 1) / kLength;
-  return n < 3 ? 1 : n;
-}
-int64_t splits_of(int64_t T, int32_t V) {
-  if (T >= kFull) return 1;
-  const int64_t want = (kParts + T - 1) / T;
-  return want < most_splits(V) ? want : most_splits(V);
-}
-
 }  // namespace
 
-// (Rows times splits never pass kParts + T - 1 with T < kFull, nor T times the
-// most splits: a bound that does not fall as T grows.)
 size_t logprobs_workspace(int64_t T, int32_t V, int32_t top_k) {
-  if (most_splits(V) < 2) return 0;
-  const int64_t parts = T * most_splits(V) < 2 * kParts ? T * most_splits(V) : 2 * kParts;
-  return static_cast<size_t>(parts) * part_bytes(top_k);
+  return static_cast<size_t>(logprobs_parts(T, V)) * part_bytes(top_k);
 }
 
 hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t s) {
-  const int splits = static_cast<int>(splits_of(a.T, a.V));
-  const int length = ((a.V + splits - 1) / splits + kStep - 1) / kStep * kStep;
+  const LogprobsPlan plan = logprobs_plan(a.T, a.V);
+  const int splits = plan.splits;
   auto go = [&](auto t) {
     using T = decltype(t);
     auto with = [&](auto wc, auto tc) {
@@ -664,13 +641,11 @@ hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t s) {
       constexpr int per = W > 4 ? 1 : 4 / W;
       const int64_t parts = a.T * splits;
       logprobs_kernel<T, W, decltype(tc)::value>
-          <<<static_cast<unsigned>((parts + per - 1) / per), W > 4 ? W * 64 : kNT, 0, s>>>(a, splits, length);
+          <<<static_cast<unsigned>((parts + per - 1) / per), W > 4 ? W * 64 : kNT, 0, s>>>(a, splits, plan.length);
     };
     auto waves = [&](auto tc) {
-      // (a wave per row, of one step or where there are rows for all waves:
-      // 4000 x 4096 bf16 16.2 us, four waves 18.9; 1000 x 4096 11.1 : 8.6)
-      if (a.V <= kStep || (a.V <= 4 * kStep && a.T >= 2048)) with(std::integral_constant<int, 1>{}, tc);
-      else if (splits == 1 && a.T < kLongFew && a.V >= 16 * kStep) with(std::integral_constant<int, 16>{}, tc);
+      if (plan.waves == 1) with(std::integral_constant<int, 1>{}, tc);
+      else if (plan.waves == 16) with(std::integral_constant<int, 16>{}, tc);
       else with(std::integral_constant<int, 4>{}, tc);
     };
     if (a.top_k > 0) waves(std::true_type{});
