@@ -47,4 +47,7 @@ inline Q8Form q8_form(int64_t M, int64_t N, int64_t K, bool on16) {
   return kQ8Tile256;
 }
 
+// kQ8Any's tiles: 128 x 128, or 64 x 64 where those leave CUs without one.
+inline int q8_any_tile(int64_t M, int64_t N) { return q8_tiles(M, N, 128) >= 256 ? 128 : 64; }
+
 }  // namespace bnn

@@ -129,8 +129,7 @@ hipError_t launch_q8gemm(const Q8Args& a, hipStream_t s) {
       q8_any_kernel<decltype(t), TS, TS><<<static_cast<unsigned>(tiles), kNT, 0, s>>>(a);
     });
   };
-  // (tiles of 64 where those of 128 leave CUs without one)
-  if (q8_tiles(a.M, a.N, 128) >= 256) any(std::integral_constant<int, 2>{});
+  if (q8_any_tile(a.M, a.N) == 128) any(std::integral_constant<int, 2>{});
   else any(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
