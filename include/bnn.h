@@ -735,7 +735,7 @@ typedef struct bnn_q8gemm_desc {
  *   y        [M][N].
  * Values of -128 are as good as any.  Rows may lie anywhere; where x and w are
  * 16-byte aligned and their strides a multiple of 16 (as bnn_rmsnorm's binding
- * lays out q), large products are quicker.  What lies between the rows is never
+ * lays out q; a single row's stride does not count), large products are quicker.  What lies between the rows is never
  * used.
  * M >= 0 (0 launches nothing), M < 2^24, 1 <= N <= 2^20, 1 <= K <= 131071,
  * M * N <= 2^35, strides <= 2^31.  Errors: BNN_ERR_NULL, BNN_ERR_SHAPE,

@@ -18,7 +18,13 @@ enum Q8Form {
 // Tiles of n x n of an M x N product.
 inline int64_t q8_tiles(int64_t M, int64_t N, int n) { return (M + n - 1) / n * ((N + n - 1) / n); }
 
-// on16: x, w and their strides on 16-byte steps.
+// Whether an operand's rows start on 16-byte steps.  (One row has no next one:
+// its distance says nothing.)
+inline bool q8_on16(uintptr_t address, int64_t stride, int64_t rows) {
+  return address % 16 == 0 && (rows == 1 || stride % 16 == 0);
+}
+
+// on16: x's and w's rows on 16-byte steps.
 //
 // Many rows: the tile whose estimated time is least, in tenths of us at K = 4096,
 // from products of 256..8192 rows.  Tiles of 64 take 3 + 7 per 256 of them (256:

@@ -116,10 +116,9 @@ __global__ __launch_bounds__(kNT) void q8_any_kernel(Q8Args a) {
 }  // namespace
 
 hipError_t launch_q8gemm(const Q8Args& a, hipStream_t s) {
-  auto on16 = [](const void* p, int64_t stride) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0;
-  };
-  const Q8Form form = q8_form(a.M, a.N, a.K, on16(a.x, a.x_stride) && on16(a.w, a.w_stride));
+  const bool on16 = q8_on16(reinterpret_cast<uintptr_t>(a.x), a.x_stride, a.M) &&
+                    q8_on16(reinterpret_cast<uintptr_t>(a.w), a.w_stride, a.N);
+  const Q8Form form = q8_form(a.M, a.N, a.K, on16);
   if (form == kQ8Skinny) return launch_q8_skinny(a, s);
   if (form != kQ8Any) return launch_q8_tile(a, form, s);
   auto any = [&](auto size) {

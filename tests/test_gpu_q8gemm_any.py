@@ -32,3 +32,12 @@ def test_types_and_options(M, N, kind):
     _check(M, N, 1024, kind, w_at=(1024, 8))
     _check(M, N, 1024, kind, bias=False, w_at=(1032, 0))
     _check(M, N, 1024, kind, scales=False, x_at=(1025, 0))
+
+
+@pytest.mark.parametrize("M, N, K", [(1, 70, 10001), (1, 4100, 8209), (300, 1, 1001), (2000, 1, 15), (1, 1, 20000)])
+def test_one_row(M, N, K):
+    """A single row whose distance is odd, on a 16-byte step and off it, with
+    nothing of its buffer behind it."""
+    pad = (K + 15) // 16 * 16
+    for first in (0, 16, 5):
+        _check(M, N, K, x_at=(K if M == 1 else pad, first if M == 1 else 0), w_at=(K if N == 1 else pad, first if N == 1 else 0))

@@ -12,6 +12,7 @@ import tile_plans
 SHIM = r"""
 #include "q8_plans.hpp"
 extern "C" int form(int64_t M, int64_t N, int64_t K, int on16) { return bnn::q8_form(M, N, K, on16); }
+extern "C" int on16(int64_t at, int64_t stride, int64_t rows) { return bnn::q8_on16(at, stride, rows); }
 extern "C" int tile(int64_t M, int64_t N) { return bnn::q8_any_tile(M, N); }
 """
 
@@ -52,3 +53,9 @@ def test_launches_fit():
         N = min(1 << 20, (1 << 35) // M)
         tile = _tile(M, N)
         assert -(-M // tile) * -(-N // tile) * 256 < 1 << 32
+
+
+def test_one_row_has_no_distance():
+    on16 = lambda *a: bool(lib().on16(*map(ctypes.c_int64, a)))  # noqa: E731
+    assert on16(0x1000, 14335, 1) and on16(0x1000, 14336, 2) and on16(0x10, 16, 9)
+    assert not on16(0x1000, 14335, 2) and not on16(0x1008, 14336, 2) and not on16(0x1001, 14335, 1)
