@@ -139,6 +139,12 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4 * (TM * TN < 8 ? 2 : 1)) 
   const float ws = a.w_scale ? a.w_scale[own] : 1.0f;
   const float bias = a.bias ? a.bias[own] : 0.0f;
 
+  // Loads that go straight to LDS count as loads from memory: a barrier alone says
+  // nothing about them, so their wait stands here, before it.
+  auto meet_all = [&]() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
   constexpr int kAhead = kStageAhead ? S : S - 1;  // stages on their way at a stage's start
 #pragma unroll
   for (int st = 0; st < kAhead; ++st) {
@@ -147,7 +153,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4 * (TM * TN < 8 ? 2 : 1)) 
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) fetch(st, st, l);
   }
-  __syncthreads();
+  meet_all();
   if (ragged && whole == 0) write_ends(0);
 #pragma unroll
   for (int s = 0; s < (kStageAhead ? kSteps : 1); ++s)
@@ -159,7 +165,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4 * (TM * TN < 8 ? 2 : 1)) 
     if (counted && S > 2)
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * kLoads) : "memory");
     else
-      __syncthreads();
+      meet_all();
   };
   // Stage `it`, in buffer st.  Main: stage it + kAhead is a whole one, and
   // fetched between the products.
