@@ -54,6 +54,10 @@ def _compile(src: str, extra=()) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("hipcc failed for %s:\n%s\n%s" % (src, " ".join(cmd), r.stderr))
+    # (hipcc's host pass does not know the feature that its device pass takes)
+    told = [line for line in r.stderr.splitlines() if "packed-fp32-ops" not in line]
+    if told:
+        print("%s:\n%s" % (src, "\n".join(told)), file=sys.stderr)
     return obj
 
 

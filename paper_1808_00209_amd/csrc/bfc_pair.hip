@@ -32,7 +32,6 @@ namespace {
 
 constexpr int kNW = 8;
 constexpr int kNT = 64 * kNW;
-constexpr int kMaxN0W = 32;  // first-layer output words (N0 <= 1024)
 constexpr uint32_t kRsrcWord3 = 0x00020000;
 
 struct FpArgs {

@@ -40,8 +40,15 @@ typedef const __attribute__((address_space(1))) void global_void;
 
 __device__ const v4i q8_zeros[1] = {{0, 0, 0, 0}};
 
+// Workgroups per CU: as many as its 160 KB of LDS hold, up to two, but one where
+// a wave's sums fill 128 registers.
+constexpr int per_cu(int TM, int TN, int WM, int WN, int S) {
+  const int lds = S * 32 * (WM * TM + WN * TN) * kBK;
+  return TM * TN < 8 && 2 * lds <= 160 * 1024 ? 2 : 1;
+}
+
 template <class T, int TM, int TN, int WM, int WN, int S>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4 * (TM * TN < 8 ? 2 : 1)) void q8_tile_kernel(
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4 * per_cu(TM, TN, WM, WN, S)) void q8_tile_kernel(
     Q8Args a, int cols, int tiles, int per_xcd, int band) {
   constexpr int kNT = 64 * WM * WN;
   constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN, kRows = BM + BN;
