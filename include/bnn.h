@@ -695,7 +695,8 @@ typedef struct bnn_rmsnorm_desc {
  *   nearest, ties to even: -127..127 (all 0, and scale 0, in a row of zeros).
  * r cancels in q, which is rounded from the exact h * weight: the same whatever
  * the order of the sums.  r and scale are good to a few units of fp32, y is
- * rounded once more to dtype.  A row whose h holds an infinity or NaN: scale
+ * rounded once more to dtype (and may lose bits where it is 2^43 times smaller
+ * than the row's largest).  A row whose h holds an infinity or NaN: scale
  * and y NaN, q 0.  weight must be finite (or else q, scale and y of the rows
  * are unspecified).
  *   x        [M][D], rows x_stride elements apart (x_stride >= D).
