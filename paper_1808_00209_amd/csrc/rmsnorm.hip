@@ -11,7 +11,7 @@
 //
 // Rows and weights of 16 bits: p is exact in fp32 (8 + 8 or 11 + 11 bits), and so
 // is its largest; sums and quotients are fp32's, as long as the largest p, the
-// sum of squares lie well inside its range (only p's that are 2^43 times
+// sum of squares and eps lie well inside its range (only p's that are 2^43 times
 // smaller than the largest may lie below it, and y lose bits there).  Other rows
 // (infinities, NaN and rows of zeros among them), and rows or weights of fp32, go
 // in 64 bits.
@@ -208,8 +208,9 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void rmsnorm_kernel(NormArgs 
       ss += sq;
     }
     row_totals<W>(ss, top, totals);
-    if (ss > 1e-25f && ss < 1e37f && top > 1e-25f && top < 1e37f) {
-      const float rstd = 1.0f / __builtin_sqrtf(ss / static_cast<float>(D) + a.eps);
+    const float mean = ss / static_cast<float>(D) + a.eps;
+    if (ss > 1e-25f && mean < 1e37f && top > 1e-25f && top < 1e37f) {
+      const float rstd = 1.0f / __builtin_sqrtf(mean);
       // (the largest |y| may lie beyond fp32 where its 127th part does not)
       const float most = top * rstd;
       if (a.q && lane == 0) a.scale[m] = most < __builtin_inff() ? most / 127.0f : top / 127.0f * rstd;

@@ -1,6 +1,6 @@
 """The norm where single steps of the formula leave fp32's range and its results
-do not: weights whose |y| passes it and whose scale, |y| / 127, does not.
-Tolerances: test_gpu_rmsnorm."""
+do not: weights whose |y| passes it and whose scale, |y| / 127, does not; an eps
+near its end.  Tolerances: test_gpu_rmsnorm."""
 import pytest
 import torch
 
@@ -39,3 +39,12 @@ def test_largest_beyond_the_range(kind, D):
     x[2:4] *= 1e-7  # (so that h w stays within fp32 for every row)
     beyond = _check(x.to(TYPES[kind]), weight.to(TYPES[kind]), 1e-30)
     assert beyond.any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("eps", [MOST, 3.4e38, 1e37, 1e36])
+def test_large_eps(kind, eps):
+    g = torch.Generator().manual_seed(7)
+    for D in (8, 700, 3000):
+        x = 3e17 * (1 + torch.rand(4, D, generator=g))
+        _check((x * (2.0 / D ** 0.5)).to(TYPES[kind]), torch.randn(D, generator=g).to(TYPES[kind]), eps)
