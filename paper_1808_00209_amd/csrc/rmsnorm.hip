@@ -209,7 +209,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : kNT) void rmsnorm_kernel(NormArgs 
     }
     row_totals<W>(ss, top, totals);
     const float mean = ss / static_cast<float>(D) + a.eps;
-    if (ss > 1e-25f && mean < 1e37f && top > 1e-25f && top < 1e37f) {
+    if (ss > 1e-25f && ss < 1e37f && mean < 1e37f && top > 1e-25f && top < 1e37f) {
       const float rstd = 1.0f / __builtin_sqrtf(mean);
       // (the largest |y| may lie beyond fp32 where its 127th part does not)
       const float most = top * rstd;
