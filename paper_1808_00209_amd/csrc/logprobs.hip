@@ -15,12 +15,12 @@
 // (the first step, rising rows), the bound is first raised to what top_k lanes'
 // largest values reach, and what still passes is placed by counting.  Values that
 // equal a full list's last key are looked at only where their index may be lower
-// (4096 rows of 32768 equal values 102 us, 2990 without; random ones 103).
+// (4096 rows of 32768 equal fp32 values 101 us, 2990 without; random ones 101).
 //
 // 4096 x 131072 bf16, 8 alternatives: 193-210 us from card to card, 5.1 to 5.5
-// TB/s, a large copy's rate (without alternatives 200 where it took 210): bound
-// by memory, the vector ALU 88 % busy.  16384 x 1000 int32, 5 alternatives:
-// 22.6-25 us, 14 without: a wave per row, 453 vector and 415 scalar instructions
+// TB/s, a large copy's rate (without alternatives 183 where it took 193): bound
+// by memory, the vector ALU 91 % busy.  16384 x 1000 int32, 5 alternatives:
+// 22.6-25 us, 12.7 without: a wave per row, 470 vector and 451 scalar instructions
 // of which the sums are 200.  301 x 50021 fp32, 8 alternatives: 20 us, 14
 // without: 1.2 rows per CU, of 16 waves that each fill a list.  One row of 65536:
 // 11.6 us in two launches, chains of dependent steps.  Tried and dropped: values

@@ -1,8 +1,10 @@
 // Root-mean-square norm with the residual's addition and an output in 8 bits
 // (bnn_rmsnorm).  One pass: a row stays in the registers of its W waves, 8
 // values at a time per lane, from the sum of squares and the largest |h w| to
-// the rounding.  Bound by memory: 8192 x 4096 bf16 with a residual in 45.8 us,
-// 5.1 TB/s (a large copy's rate on this card), fp32 in 88 us, 5.0 TB/s.
+// the rounding.  Bound by memory: 8192 x 4096 bf16 with a residual in 42-50 us
+// from card to card (45.8: 5.1 TB/s, a large copy's rate), fp32 in 84-88 us, 5.0
+// to 5.2 TB/s.  16-bit rows under fp32 weights go in 64 bits throughout and are
+// bound by those: 59-62 us, 3.8 to 4.0 TB/s.
 //
 // r cancels in q = rint(127 p / max p), p = h w, which is rounded as if from the
 // exact p: where the quotient comes near a border n + 1/2 (within 2^-13, many
