@@ -32,9 +32,9 @@ inline bool q8_on16(uintptr_t address, int64_t stride, int64_t rows) {
 // 22.9); two per CU and more of these 28 + 10 (280: 29.6, 420: 36), then 38 per
 // round of 512; tiles of 256 58 per round (up to half a round 46, the clock being
 // higher).  Other K move all of them alike, but small ones favour fewer tiles
-// (1500 x 3000, K 700: 64 13.7, two of 128 per CU 10.5 us; K 4096: 33.2, 28.2).  Of
+// (1500 x 3000, K 700: 64 13.6, two of 128 per CU 10.6 us; K 4096: 32.3, 27.1).  Of
 // 46 products with K of 400 to 28672 two are off the best tile (64 x 20000, K 8000
-// 1.16, 1500 x 1500, K 512 1.12), the others within 1.01.
+// 1.16, 1500 x 1500, K 512 1.11), the others within 1.01.
 //
 // Few rows (us, skinny : tiles of 64, K 4096): 16 rows of 4096 outputs 8.0 : 8.7
 // and of 65536 58.0 : 59.4; 32 rows, in two operands of the skinny kernel, 10.6 :
